@@ -134,7 +134,7 @@ def _stored(x, store):
         return x.to(STORE[store]), None
     big = x.float().abs().amax(-1)
     if store == "i8":
-        scale = (big / 127).clamp_min(2.0 ** -126)
+        scale = (big.double() / 127).float().clamp_min(2.0 ** -126)
         return torch.round(x.double() / scale.double()[..., None]).clamp(-127, 127).to(torch.int8), scale  # borders need 64 bits
     m, e = torch.frexp(big.double())  # big = m * 2^e, m in [0.5, 1); 448 = 0.875 * 2^9
     k = (e - 9 + (m > 0.875)).clamp_min(-126)
