@@ -42,9 +42,10 @@ enum {
 };
 
 enum { MDI_ARCH_GPT = 0, MDI_ARCH_LLAMA = 1 };
-enum { MDI_DTYPE_F32 = 0, MDI_DTYPE_BF16 = 1 };
+enum { MDI_DTYPE_F32 = 0, MDI_DTYPE_BF16 = 1, MDI_DTYPE_F16 = 2 }; /* F16: rows given to the operators only, not weights */
 enum { MDI_ACT_GELU_TANH = 0, MDI_ACT_GELU_ERF = 1, MDI_ACT_SWIGLU = 2 };
-enum { MDI_KV_DEFAULT = 0, MDI_KV_BF16 = 1, MDI_KV_F16 = 2, MDI_KV_F32 = 3 };
+enum { MDI_KV_DEFAULT = 0, MDI_KV_BF16 = 1, MDI_KV_F16 = 2, MDI_KV_F32 = 3,
+       MDI_KV_I8 = 4, MDI_KV_E4M3 = 5 }; /* 8-bit elements with one fp32 scale per row and head; see mdi_kv_cache */
 
 typedef struct mdi_ctx mdi_ctx;
 
@@ -263,8 +264,83 @@ int mdi_sync(mdi_ctx *ctx);
  * text is available from mdi_last_error(NULL). */
 int mdi_greedy_argmax_static(const float *logits_dev, int n_rows, int n_cols, int32_t *out_dev, void *stream);
 
+/* ---- Operators on the caller's own device memory ------------------------------------------------------------
+ * The paged key/value cache, what fills it and what reads it, without a context: for callers who run their own
+ * layers and scheduler.  Every pointer named *_dev, and data_dev / pool_dev / scale_dev inside the structures, is
+ * device memory of the current device (anything else is refused with MDI_ERR_ARG); the structures themselves are
+ * host memory and are read before the call returns.  The work is enqueued on `stream` (a cudaStream_t, NULL = default
+ * stream) and can be captured into a CUDA graph; nothing is allocated, nothing is kept from one call to the next, and
+ * results do not depend on timing (the same call gives the same bits).  Errors: ARG, SHAPE, CUDA; the text is available
+ * from mdi_last_error(NULL).  What only the device knows (lengths, positions, page numbers) is checked there:
+ * nothing outside the given ranges is read or written, and with status_dev (one int32, or NULL) the bits of
+ * MDI_STATUS_* are OR-ed into *status_dev, which the caller clears. */
+enum {
+    MDI_STATUS_PAGE = 1,   /* a page number outside [0, n_pages): its rows were not written / read as zeros / left out of the attention */
+    MDI_STATUS_RANGE = 2,  /* a position, length or slot outside the page table, or row offsets that do not ascend: the part outside was left out */
+    MDI_STATUS_TIMEOUT = 4 /* a bounded wait inside a kernel ran out: the results of the call are not complete */
+};
+
+/* Rows of heads: element e of head h of row r is data_dev[r * row_stride + h * head_stride + e] (strides in elements,
+ * so that q, k and v can be parts of one projection's output).  data_dev and both strides must be multiples of 16 bytes. */
+typedef struct {
+    void *data_dev;
+    int dtype;                       /* MDI_DTYPE_* */
+    int64_t row_stride, head_stride;
+} mdi_rows;
+
+/* A paged cache.  Page = [keys | values][n_kv_head][page_tokens][head_dim] elements of dtype; position t of a sequence in
+ * page-table row `slot` is row t % page_tokens of page page_table[slot][t / page_tokens].
+ * dtype: MDI_KV_F16, MDI_KV_BF16, or 8 bits per element with one fp32 scale per row of a head, [n_pages][2][n_kv_head][page_tokens]:
+ *   MDI_KV_I8:   scale = max(absmax / 127, 2^-126), element = x / scale rounded to the nearest integer, ties to even;
+ *   MDI_KV_E4M3: scale = 2^k, the smallest k >= -126 with absmax <= 448 * 2^k, element = x / scale rounded to e4m3.
+ * The element stands for element * scale.  A row that holds an infinity or a NaN reads back as NaN throughout (8-bit types). */
+typedef struct {
+    void *pool_dev;                  /* [n_pages][2][n_kv_head][page_tokens][head_dim], 16-byte aligned */
+    float *scale_dev;                /* [n_pages][2][n_kv_head][page_tokens], 16-byte aligned; 8-bit types only (else ignored) */
+    const int32_t *page_table_dev;   /* [n_slots][page_table_stride] */
+    int64_t page_table_stride;       /* entries from one slot's row to the next, >= pages_per_seq */
+    int n_pages, n_slots, pages_per_seq;
+    int page_tokens;                 /* rows per page: a power of two >= 16 */
+    int n_kv_head, head_dim;         /* head_dim: 16, 32, 64 or 128; n_kv_head <= 1024 */
+    int dtype;                       /* MDI_KV_F16, MDI_KV_BF16, MDI_KV_I8 or MDI_KV_E4M3 */
+} mdi_kv_cache;
+
+/* Write new rows into the cache (Section III-D: the cached matrices are extended).  k, v: packed rows of n_kv_head heads, any
+ * dtype; rows seq_start_dev[i] .. seq_start_dev[i+1]-1 belong to sequence i of n_seq and go to positions pos_dev[i] and
+ * following of its slot.  seq_start_dev: [n_seq+1]; n_rows: rows that k and v hold; rows at or behind
+ * seq_start_dev[n_seq] are not read.  slot_dev: page-table row of each sequence, NULL: sequence i has slot i.
+ * Two rows of one call must not go to the same place. */
+int mdi_kv_append(const mdi_kv_cache *cache, int n_seq, const int32_t *slot_dev, const int32_t *seq_start_dev, const int32_t *pos_dev,
+                  int n_rows, const mdi_rows *k, const mdi_rows *v, int32_t *status_dev, void *stream);
+
+/* The way back: cached rows as packed k_out, v_out of any dtype (element * scale in fp32, rounded to dtype).  pos_dev: first position of
+ * each sequence, NULL: 0.  Output rows at or behind seq_start_dev[n_seq] are left as they are. */
+int mdi_kv_read(const mdi_kv_cache *cache, int n_seq, const int32_t *slot_dev, const int32_t *seq_start_dev, const int32_t *pos_dev,
+                int n_rows, const mdi_rows *k_out, const mdi_rows *v_out, int32_t *status_dev, void *stream);
+
+/* Attention of one new token per sequence over the cached rows 0 .. len_dev[i]-1 of its slot (its own row already appended):
+ * out[i][h] = sum_j softmax_j(scale * q[i][h] . K_j) V_j with K, V of key/value head h / (n_head / n_kv_head).  q, out: n_seq
+ * rows of n_head heads, of the same dtype.  len 0 gives zeros.  max_len: an upper bound of the lengths (0: what the page
+ * table can hold); it only decides over how many blocks a sequence is split, longer sequences are still read whole.
+ * workspace_dev: mdi_attn_decode_workspace() bytes (its contents do not matter), 16-byte aligned, used by one call at a
+ * time.  scale > 0. */
+int64_t mdi_attn_decode_workspace(const mdi_kv_cache *cache, int n_seq, int n_head, int max_len);
+int mdi_attn_decode(const mdi_kv_cache *cache, int n_seq, const int32_t *slot_dev, const int32_t *len_dev, int max_len, int n_head,
+                    const mdi_rows *q, const mdi_rows *out, float scale, void *workspace_dev, int64_t workspace_bytes,
+                    int32_t *status_dev, void *stream);
+
+/* Causal attention over packed sequences (first visits: whole prompts, or the next chunk of a prompt behind rows that are cached
+ * already).  Sequence i: query rows q_start_dev[i] .. q_start_dev[i+1]-1 of q, key/value rows k_start_dev[i] .. k_start_dev[i+1]-1 of
+ * k and v.  Its last query row sees all its keys, the one before all but the last, and so on; a row that sees nothing
+ * (more queries than keys) gives zeros.  n_q_rows, n_k_rows: rows that q / out and k / v hold; rows of out at or behind
+ * q_start_dev[n_seq] are left as they are.  q, k, v, out: one dtype, F16 or BF16; head_dim 16, 32, 64 or 128; n_head a multiple of
+ * n_kv_head.  The weights are rounded to that dtype before they meet the values, sums are fp32.  scale > 0. */
+int mdi_attn_prompt(int n_seq, const int32_t *q_start_dev, const int32_t *k_start_dev, int n_q_rows, int n_k_rows, int n_head, int n_kv_head,
+                    int head_dim, const mdi_rows *q, const mdi_rows *k, const mdi_rows *v, const mdi_rows *out, float scale,
+                    int32_t *status_dev, void *stream);
+
 /* Text of the last error of this context; with ctx NULL, of the last failed call that takes no context
- * (mdi_create, mdi_greedy_argmax_static). */
+ * (mdi_create, mdi_greedy_argmax_static, the operators). */
 const char *mdi_last_error(mdi_ctx *ctx);
 
 #ifdef __cplusplus

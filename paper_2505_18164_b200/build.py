@@ -12,7 +12,7 @@ LIB_MDI = os.path.join(_HERE, "libmdi.so")
 LIB_INPUTS = os.path.join(_HERE, "libmdi_inputs.so")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-Xcompiler", "-fPIC", "-shared"]
+              "-Xcompiler", "-fPIC", "-shared", "-t", "0"]
 
 
 def _stale(target: str, sources) -> bool:

@@ -17,14 +17,16 @@ LIB_PATH = os.path.join(_HERE, "libmdi.so")
 
 MDI_OK = 0
 TRACE_WORDS = 128
-KV_DEFAULT, KV_BF16, KV_F16, KV_F32 = 0, 1, 2, 3
+KV_DEFAULT, KV_BF16, KV_F16, KV_F32, KV_I8, KV_E4M3 = 0, 1, 2, 3, 4, 5
+STATUS_PAGE, STATUS_RANGE, STATUS_TIMEOUT = 1, 2, 4
 ERR_ARG, ERR_SHAPE, ERR_OOM, ERR_CONTEXT, ERR_STATE, ERR_TIMEOUT, ERR_CUDA = -1, -2, -3, -4, -5, -6, -7
 _ERR_NAMES = {ERR_ARG: "MDI_ERR_ARG", ERR_SHAPE: "MDI_ERR_SHAPE", ERR_OOM: "MDI_ERR_OOM", ERR_CONTEXT: "MDI_ERR_CONTEXT",
               ERR_STATE: "MDI_ERR_STATE", ERR_TIMEOUT: "MDI_ERR_TIMEOUT", ERR_CUDA: "MDI_ERR_CUDA"}
 
 EXPORTS = ["mdi_create", "mdi_destroy", "mdi_load_weights", "mdi_prefill", "mdi_prefill_dev", "mdi_step",
            "mdi_generate", "mdi_generate_dev", "mdi_get_logits", "mdi_set_sampling", "mdi_set_teacher_tokens", "mdi_reset_sample",
-           "mdi_get_stats", "mdi_get_partition_times", "mdi_get_trace", "mdi_memory_bytes", "mdi_sync", "mdi_last_error", "mdi_greedy_argmax_static"]
+           "mdi_get_stats", "mdi_get_partition_times", "mdi_get_trace", "mdi_memory_bytes", "mdi_sync", "mdi_last_error", "mdi_greedy_argmax_static",
+           "mdi_kv_append", "mdi_kv_read", "mdi_attn_decode_workspace", "mdi_attn_decode", "mdi_attn_prompt"]
 
 
 class MdiError(RuntimeError):
@@ -54,6 +56,16 @@ class Stats(ctypes.Structure):
                 ("stage_steps", ctypes.c_int64), ("kernel_launches", ctypes.c_int64),
                 ("last_prefill_ms", ctypes.c_float), ("last_generate_ms", ctypes.c_float),
                 ("last_run_ms", ctypes.c_float), ("kv_element_bytes", ctypes.c_int)]
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("data_dev", ctypes.c_void_p), ("dtype", ctypes.c_int), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class KvCacheStruct(ctypes.Structure):
+    _fields_ = [("pool_dev", ctypes.c_void_p), ("scale_dev", ctypes.c_void_p), ("page_table_dev", ctypes.c_void_p),
+                ("page_table_stride", ctypes.c_int64)] + \
+               [(n, ctypes.c_int) for n in ("n_pages", "n_slots", "pages_per_seq", "page_tokens", "n_kv_head", "head_dim", "dtype")]
 
 
 _lib = None
@@ -88,6 +100,13 @@ def lib():
         L.mdi_memory_bytes.restype = ctypes.c_int64
         L.mdi_sync.argtypes = [vp]
         L.mdi_greedy_argmax_static.argtypes = [vp, ci, ci, vp, vp]
+        i64, rows, cache = ctypes.c_int64, ctypes.POINTER(Rows), ctypes.POINTER(KvCacheStruct)
+        L.mdi_kv_append.argtypes = [cache, ci, vp, vp, vp, ci, rows, rows, vp, vp]
+        L.mdi_kv_read.argtypes = [cache, ci, vp, vp, vp, ci, rows, rows, vp, vp]
+        L.mdi_attn_decode_workspace.argtypes = [cache, ci, ci, ci]
+        L.mdi_attn_decode_workspace.restype = i64
+        L.mdi_attn_decode.argtypes = [cache, ci, vp, vp, ci, ci, rows, rows, ctypes.c_float, vp, i64, vp, vp]
+        L.mdi_attn_prompt.argtypes = [ci, vp, vp, ci, ci, ci, ci, ci, rows, rows, rows, rows, ctypes.c_float, vp, vp]
         L.mdi_last_error.argtypes = [vp]
         L.mdi_last_error.restype = ctypes.c_char_p
         _lib = L
@@ -111,6 +130,110 @@ def greedy_argmax_static(logits_dev, n_rows: int, n_cols: int, out_dev, stream: 
     rc = lib().mdi_greedy_argmax_static(_ptr(logits_dev), n_rows, n_cols, _ptr(out_dev), stream)
     if rc != MDI_OK:
         raise MdiError(rc, (lib().mdi_last_error(None) or b"").decode())
+
+
+# ---- operators on the caller's device tensors (see the second half of mdi.h) ------------------------------------------
+_ROW_DTYPES = {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2}
+_KV_DTYPES = {"torch.bfloat16": KV_BF16, "torch.float16": KV_F16, "torch.int8": KV_I8, "torch.float8_e4m3fn": KV_E4M3}
+
+
+def _fail_arg(text: str):
+    raise MdiError(ERR_ARG, text)
+
+
+def _op_check(rc: int):
+    if rc != MDI_OK:
+        raise MdiError(rc, (lib().mdi_last_error(None) or b"").decode())
+
+
+def _rows(name: str, t, rows: int, heads: int, head_dim: int) -> Rows:
+    """A [rows][heads][head_dim] tensor (any strides but the last) as the library's row view."""
+    dt = _ROW_DTYPES.get(str(t.dtype))
+    if dt is None:
+        _fail_arg(f"{name}: dtype {t.dtype} is none of float32, bfloat16, float16")
+    if t.dim() != 3 or t.shape[0] < rows or t.shape[1] != heads or t.shape[2] != head_dim:
+        _fail_arg(f"{name}: shape {tuple(t.shape)}, expected [{rows}][{heads}][{head_dim}]")
+    s0, s1, s2 = t.stride()
+    if s2 != 1:
+        _fail_arg(f"{name}: the elements of a head must be contiguous")
+    return Rows(t.data_ptr(), dt, s0 if rows > 1 else heads * head_dim, s1 if heads > 1 else head_dim)
+
+
+def _ints(name: str, t, n: int):
+    """Address of a device tensor of at least n int32 values (None: 0)."""
+    if t is None:
+        return 0
+    if str(t.dtype) != "torch.int32" or t.numel() < n or not t.is_contiguous():
+        _fail_arg(f"{name}: expected a contiguous int32 tensor of at least {n} elements")
+    return t.data_ptr()
+
+
+class KvCache:
+    """A paged key/value cache over the caller's device tensors (mdi_kv_cache): ``pool`` [n_pages][2][n_kv_head][page_tokens]
+    [head_dim] of float16, bfloat16, int8 or float8_e4m3fn; ``page_table`` int32 [n_slots][pages_per_seq]; ``scale`` float32
+    [n_pages][2][n_kv_head][page_tokens] for the 8-bit types.  The tensors are kept alive by this object."""
+
+    def __init__(self, pool, page_table, scale=None):
+        dt = _KV_DTYPES.get(str(pool.dtype))
+        if dt is None:
+            _fail_arg(f"pool: dtype {pool.dtype} is none of float16, bfloat16, int8, float8_e4m3fn")
+        if pool.dim() != 5 or pool.shape[1] != 2 or not pool.is_contiguous():
+            _fail_arg("pool: expected a contiguous [n_pages][2][n_kv_head][page_tokens][head_dim] tensor")
+        if str(page_table.dtype) != "torch.int32" or page_table.dim() != 2 or page_table.stride(1) != 1:
+            _fail_arg("page_table: expected int32 [n_slots][pages_per_seq]")
+        if dt in (KV_I8, KV_E4M3) and (scale is None or str(scale.dtype) != "torch.float32" or tuple(scale.shape) != tuple(pool.shape[:4])
+                                       or not scale.is_contiguous()):
+            _fail_arg("scale: 8-bit caches need a contiguous float32 [n_pages][2][n_kv_head][page_tokens] tensor")
+        self.tensors = (pool, page_table, scale)
+        self.n_slots, self.n_kv_head, self.head_dim = page_table.shape[0], pool.shape[2], pool.shape[4]
+        self._c = KvCacheStruct(pool.data_ptr(), _ptr(scale) if scale is not None else 0, page_table.data_ptr(),
+                                page_table.stride(0) if self.n_slots > 1 else max(page_table.shape[1], 1), pool.shape[0], self.n_slots, page_table.shape[1], pool.shape[3],
+                                self.n_kv_head, self.head_dim, dt)
+
+
+def kv_append(cache: KvCache, k, v, seq_start, pos, slots=None, status=None, stream: int = 0):
+    """mdi_kv_append: rows seq_start[i] .. seq_start[i+1]-1 of ``k``, ``v`` ([rows][n_kv_head][head_dim]) go to positions pos[i] ..
+    of sequence i's slot (``slots[i]``, or i)."""
+    n_seq, n = seq_start.numel() - 1, k.shape[0]
+    kr, vr = _rows("k", k, n, cache.n_kv_head, cache.head_dim), _rows("v", v, n, cache.n_kv_head, cache.head_dim)
+    _op_check(lib().mdi_kv_append(cache._c, n_seq, _ints("slots", slots, n_seq), _ints("seq_start", seq_start, n_seq + 1),
+                                  _ints("pos", pos, n_seq), n, kr, vr, _ints("status", status, 1), stream))
+
+
+def kv_read(cache: KvCache, k_out, v_out, seq_start, pos=None, slots=None, status=None, stream: int = 0):
+    """mdi_kv_read: the reverse of kv_append, into ``k_out``, ``v_out``; ``pos`` None reads every sequence from position 0."""
+    n_seq, n = seq_start.numel() - 1, k_out.shape[0]
+    kr, vr = _rows("k_out", k_out, n, cache.n_kv_head, cache.head_dim), _rows("v_out", v_out, n, cache.n_kv_head, cache.head_dim)
+    _op_check(lib().mdi_kv_read(cache._c, n_seq, _ints("slots", slots, n_seq), _ints("seq_start", seq_start, n_seq + 1),
+                                _ints("pos", pos, n_seq), n, kr, vr, _ints("status", status, 1), stream))
+
+
+def attn_decode_workspace(cache: KvCache, n_head: int, max_len: int = 0, n_seq: Optional[int] = None) -> int:
+    """Bytes of working memory of attn_decode for ``n_seq`` sequences (default: every slot)."""
+    rc = lib().mdi_attn_decode_workspace(cache._c, cache.n_slots if n_seq is None else n_seq, n_head, max_len)
+    if rc < 0:
+        _op_check(rc)
+    return rc
+
+
+def attn_decode(cache: KvCache, q, out, lens, max_len: int = 0, scale: Optional[float] = None, workspace=None, slots=None,
+                status=None, stream: int = 0):
+    """mdi_attn_decode: one new token per sequence, ``q``, ``out`` [n_seq][n_head][head_dim], over the first lens[i] cached rows.
+    ``scale``: default 1 / sqrt(head_dim).  ``workspace``: a device tensor of attn_decode_workspace() bytes."""
+    n_seq, n_head = q.shape[0], q.shape[1]
+    qr, orow = _rows("q", q, n_seq, n_head, cache.head_dim), _rows("out", out, n_seq, n_head, cache.head_dim)
+    ws = (workspace.data_ptr(), workspace.numel() * workspace.element_size()) if workspace is not None else (0, 0)
+    _op_check(lib().mdi_attn_decode(cache._c, n_seq, _ints("slots", slots, n_seq), _ints("lens", lens, n_seq), max_len, n_head, qr, orow,
+                                    cache.head_dim ** -0.5 if scale is None else scale, ws[0], ws[1], _ints("status", status, 1), stream))
+
+
+def attn_prompt(q, k, v, out, q_start, k_start, scale: Optional[float] = None, status=None, stream: int = 0):
+    """mdi_attn_prompt: causal attention over packed sequences, ``q``, ``out`` [q rows][n_head][head_dim], ``k``, ``v`` [key
+    rows][n_kv_head][head_dim]; ``q_start``, ``k_start`` int32 [n_seq + 1].  ``scale``: default 1 / sqrt(head_dim)."""
+    n_seq, (nq, n_head, hd), (nk, n_kv) = q_start.numel() - 1, q.shape, k.shape[:2]
+    r = [_rows("q", q, nq, n_head, hd), _rows("k", k, nk, n_kv, hd), _rows("v", v, nk, n_kv, hd), _rows("out", out, nq, n_head, hd)]
+    _op_check(lib().mdi_attn_prompt(n_seq, _ints("q_start", q_start, n_seq + 1), _ints("k_start", k_start, n_seq + 1), nq, nk, n_head, n_kv, hd,
+                                    r[0], r[1], r[2], r[3], hd ** -0.5 if scale is None else scale, _ints("status", status, 1), stream))
 
 
 class Context:
