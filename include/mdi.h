@@ -320,7 +320,8 @@ int mdi_kv_read(const mdi_kv_cache *cache, int n_seq, const int32_t *slot_dev, c
 
 /* Attention of one new token per sequence over the cached rows 0 .. len_dev[i]-1 of its slot (its own row already appended):
  * out[i][h] = sum_j softmax_j(scale * q[i][h] . K_j) V_j with K, V of key/value head h / (n_head / n_kv_head).  q, out: n_seq
- * rows of n_head heads, of the same dtype.  len 0 gives zeros.  max_len: an upper bound of the lengths (0: what the page
+ * rows of n_head heads, of the same dtype.  len 0 gives zeros; an infinity among the values gives NaN in its
+ * element of the output.  max_len: an upper bound of the lengths (0: what the page
  * table can hold); it only decides over how many blocks a sequence is split, longer sequences are still read whole.
  * workspace_dev: mdi_attn_decode_workspace() bytes (its contents do not matter), 16-byte aligned, used by one call at a
  * time.  scale > 0. */
