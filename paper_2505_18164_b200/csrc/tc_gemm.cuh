@@ -11,7 +11,8 @@
 // Every wait is bounded in wall time; on a timeout an error word is set, the block skips the remaining
 // waits, frees its tensor memory and returns.
 #pragma once
-#include <cuda.h>
+#include "tc_prims.cuh"
+
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -58,18 +59,6 @@ struct TgArgs {
     __nv_bfloat16 *out_hi, *out_lo; // optional: the result also (or, with y null, only) as two bf16 planes [T][ldy]
 };
 
-__device__ __forceinline__ uint32_t tg_smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ unsigned long long tg_now() {
-    unsigned long long t;
-    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-    return t;
-}
-__device__ __forceinline__ bool tg_try_wait(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
-                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    return ok != 0;
-}
 // returns false when the wait gave up (or somebody else already did)
 __device__ __noinline__ bool tg_wait(uint32_t bar, uint32_t parity, int *err) {
     unsigned long long t0 = 0;
@@ -86,29 +75,6 @@ __device__ __noinline__ bool tg_wait(uint32_t bar, uint32_t parity, int *err) {
     return false;
 }
 
-// Shared-memory matrix descriptor of a K-major tile whose rows are 128 bytes, stored with the 128-byte
-// swizzle (what TMA wrote): start address, stride between 8-row groups = 1024 bytes, descriptor version 1,
-// layout type 2 (128-byte swizzle).  The leading-dimension offset is not used by this layout.
-__device__ __forceinline__ uint64_t tg_desc(uint32_t smem_addr) {
-    uint64_t d = 0;
-    d |= (uint64_t)((smem_addr & 0x3FFFF) >> 4);
-    d |= (uint64_t)1 << 16;
-    d |= (uint64_t)(1024 >> 4) << 32;
-    d |= (uint64_t)1 << 46;
-    d |= (uint64_t)2 << 61;
-    return d;
-}
-// Instruction descriptor, kind::f16: D fp32, A and B bf16, both K-major, N and M as given.
-__device__ __forceinline__ uint32_t tg_idesc(int m, int n) {
-    return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
-}
-__device__ __forceinline__ void tg_mma(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
-                 ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
-}
-__device__ __forceinline__ void tg_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
 __device__ __forceinline__ void tg_tma_2d(uint32_t dst, const CUtensorMap *map, int c0, int c1, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                  ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(bar) : "memory");
@@ -280,22 +246,7 @@ __global__ void k_tile_weights(const __nv_bfloat16 *w, int n_rows, int K, __nv_b
 }
 
 // Host: 2-D tensor map over a row-major bf16 matrix [rows][cols] with a box of box_rows x 64 columns,
-// 128-byte swizzle, zero fill outside.  cols * 2 must be a multiple of 16 bytes.  The driver's encoder is
-// looked up at run time through the runtime API, so that the library does not link against the driver
-// (and still loads on a machine without one).
-typedef CUresult (*tg_encode_fn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-inline tg_encode_fn tg_encoder() {
-    static tg_encode_fn fn = nullptr;
-    if (!fn) {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess)
-            fn = reinterpret_cast<tg_encode_fn>(p);
-    }
-    return fn;
-}
+// 128-byte swizzle, zero fill outside.  cols * 2 must be a multiple of 16 bytes.
 inline CUresult tg_make_map(CUtensorMap *map, const void *base, uint64_t rows, uint64_t cols, uint32_t box_rows) {
     const tg_encode_fn enc = tg_encoder();
     if (!enc) return CUDA_ERROR_NOT_SUPPORTED;

@@ -558,6 +558,22 @@ def test_prompt_rows_past_32_bits():
     assert torch.equal(q, b)
 
 
+def test_prompt_head_major_rows_and_broadcast():
+    """[head][row][element] tensors; a stride of zero is refused."""
+    n, heads, kv, hd = 333, 4, 2, 64
+    q, k, v = (torch.randn(h, n, hd, generator=gen(h), device=DEV).to(BF16).transpose(0, 1) for h in (heads, kv, kv))
+    buf = torch.zeros(heads, n, hd, dtype=BF16, device=DEV)
+    mdi.attn_prompt(q, k, v, buf.transpose(0, 1), starts([n]), starts([n]))
+    out = torch.empty(n, heads, hd, dtype=BF16, device=DEV)
+    mdi.attn_prompt(q.contiguous(), k.contiguous(), v.contiguous(), out, starts([n]), starts([n]))
+    assert torch.equal(buf.transpose(0, 1), out)
+    check_prompt(q, k, v, out, [n], [n], BF16)
+    for x in (k[:, :1].expand(n, kv, hd), k[:1].expand(n, kv, hd)):
+        with pytest.raises(mdi.MdiError) as e:
+            mdi.attn_prompt(q, x, v, out, starts([n]), starts([n]))
+        assert e.value.code == mdi.ERR_SHAPE
+
+
 def test_prompt_in_a_graph_with_other_lengths():
     nq, nk = [300, 212], [300, 212]
     q, k, v = prompt_case(BF16, 4, 2, 128, nq, nk, seed=5)

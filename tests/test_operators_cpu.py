@@ -88,6 +88,7 @@ def test_prompt():
     assert code(mdi.attn_prompt, q, k, k, q, ints(0, 5), ints(0)) == mdi.ERR_ARG
     for s in (0.0, -0.5, float("nan"), float("inf")):
         assert code(mdi.attn_prompt, q, k, k, q, *one, scale=s) == mdi.ERR_ARG
+    assert code(mdi.attn_prompt, q, k[:, :1].expand(7, 2, 64), k, q, *one) in (mdi.ERR_SHAPE, mdi.ERR_ARG, mdi.ERR_CUDA)
     odd = torch.zeros(7, 2, 68, dtype=BF16)[:, :, :64]
     assert code(mdi.attn_prompt, q, odd, k, q, *one) == mdi.ERR_SHAPE
     assert code(mdi.attn_prompt, q, k, k, q, *one) in (mdi.ERR_ARG, mdi.ERR_CUDA)
