@@ -2,13 +2,15 @@
 //     out[i][h] = sum_j softmax_j(scale * q[i][h] . K_j) V_j,   j < len[i],   K, V of key/value head h / group.
 //
 // Bound: the bytes of the cached rows.  What the layout is for:
-//  * Work is cut into tiles of 16 cached rows (a tile never crosses a page).  All tiles of all (sequence, key/value head,
+//  * Work is cut into tiles of cached rows: 16 (16-bit types) or 32 (8-bit types: as many bytes; one softmax step serves
+//    twice the rows), in units of 16 that never cross a page.  All tiles of all (sequence, key/value head,
 //    chunk of up to 8 of its query heads) are laid end to end and dealt to the warps of the launch in equal contiguous
 //    shares, so sequences of any mix of lengths keep every warp equally busy.  A (sequence, head) that a share boundary
 //    cuts leaves partial results (maximum, sum, unnormalised output) in the workspace; a second, small kernel joins them in
 //    a fixed order.  Nothing depends on timing.
-//  * A warp streams its tiles through its own ring of shared memory with asynchronous copies: every lane copies exactly the
-//    bytes that it will use itself as matrix-instruction fragments, so a stage needs no barrier.
+//  * A warp streams its tiles through its own ring of shared memory with asynchronous copies of whole contiguous rows (a
+//    unit's rows of one head are contiguous in its page).  16-byte chunks are stored swizzled, so that reading fragments has
+//    no bank conflicts where rows have 128 bytes or more.  No barrier but the warp's own is needed.
 //  * Products run on the tensor cores (mma.sync m16n8k16, fp32 accumulators), not for their rate but because one
 //    instruction then serves the up to 8 query heads that share the row.  Scores: A = query (rows 0-7 the heads' high
 //    parts, rows 8-15 their low parts), B = 8 cached rows; a lane then holds the scores of head lane / 4 for cached rows
@@ -32,20 +34,31 @@ namespace {
 
 constexpr int AD_WARPS = 4;      // warps per block (they share nothing but the table of lengths)
 constexpr int AD_THREADS = AD_WARPS * 32;
-constexpr int AD_STAGES = 3;
+#ifndef AD_U8
+#define AD_U8 2
+#define AD_U16 2
+#endif
+#ifndef AD_MAXB
+#define AD_MAXB 4
+#endif
+#ifndef AD_STAGES_DEF
+#define AD_STAGES_DEF 2
+#endif
 constexpr int AD_MAX_SEQ = 256;  // sequences per launch (their table shares shared memory with the rings of 4 blocks per SM)
 constexpr int AD_HC = 8;         // query heads per chunk
 constexpr int AD_SM = 148;
+#ifndef AD_TURN
+#define AD_TURN 2
+#endif
 constexpr float AD_SLACK = 4.f;  // a maximum may be exceeded by 2^4 before what has been summed is rescaled
-constexpr int AD_MERGE_THREADS = 128;
+constexpr int AD_JOIN_THREADS = 128;
 
 struct AdArgs {
     OpCache c;
     OpRows q, out;
     const int *len;
     int *status;
-    long long *head;  // workspace: tiles before each sequence, [n_seq + 1]
-    float *part;      // workspace: [warps][2][hc][HD + 4]: output, then maximum, sum, exponent of the weights' scale
+    float *part;      // workspace: [warps][pair from an earlier share | pair that goes on in a later one][hc][HD + 4]: output, maximum, sum, exponent of the weights' scale
     int n_seq, seq0;  // sequences of this launch, first one's number
     int n_head, group, chunks, hc, n_warps, min_tiles;
     float scale_log2e;
@@ -55,15 +68,15 @@ enum { AD_I8, AD_E4M3, AD_F16, AD_BF16 };
 template <int ST> struct AdStore {
     static constexpr int SIZE = ST <= AD_E4M3 ? 1 : 2;
     static constexpr bool SCALED = SIZE == 1, BF = ST == AD_BF16;
-    static constexpr int BLOCKS = SIZE == 1 ? 4 : 2; // resident blocks per SM
+    static constexpr int U = SIZE == 1 ? AD_U8 : AD_U16;       // 16-row units per tile
 };
 
 __device__ __forceinline__ void ad_mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, std::false_type) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void ad_mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, std::true_type) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ float ad_exp2(float x) {
@@ -116,43 +129,44 @@ template <int ST, int UPPER> __device__ __forceinline__ uint32_t ad_wide(uint32_
 }
 template <int ST> __device__ __forceinline__ uint32_t ad_bias(uint32_t w) { return ST == AD_I8 ? w ^ 0x80808080u : w; }
 
-// `bytes` (2, 4, 8 or 16) from global to shared memory, zeros where !ok
-template <int BYTES> __device__ __forceinline__ void ad_copy(uint32_t dst, const unsigned char *src, bool ok) {
-    const int n = ok ? BYTES : 0;
-    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
-    else if constexpr (BYTES == 8) asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
-    else if constexpr (BYTES == 4) asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
-    else {
-        const unsigned short v = ok ? *(const unsigned short *)src : (unsigned short)0;
-        asm volatile("st.shared.u16 [%0], %1;" ::"r"(dst), "h"(v) : "memory");
-    }
+// 16 bytes from global to shared memory, zeros where !ok
+__device__ __forceinline__ void ad_copy16(uint32_t dst, const unsigned char *src, bool ok) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
 }
-template <int BYTES> __device__ __forceinline__ void ad_read(uint32_t (&w)[(BYTES + 3) / 4], uint32_t src) {
-    if constexpr (BYTES == 16) asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(src) : "memory");
-    else if constexpr (BYTES == 8) asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(src) : "memory");
-    else if constexpr (BYTES == 4) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(src) : "memory");
-    else {
-        unsigned short v;
-        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(src) : "memory");
-        w[0] = v;
-    }
+__device__ __forceinline__ void ad_copy4(uint32_t dst, const float *src, bool ok) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(ok ? 4 : 0) : "memory");
 }
+template <int BYTES> __device__ __forceinline__ void ad_read(uint32_t (&w)[(BYTES + 3) / 4], const unsigned char *p) {
+    if constexpr (BYTES == 16) { const uint4 v = *(const uint4 *)p; w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
+    else if constexpr (BYTES == 8) { const uint2 v = *(const uint2 *)p; w[0] = v.x; w[1] = v.y; }
+    else if constexpr (BYTES == 4) w[0] = *(const uint32_t *)p;
+    else w[0] = *(const unsigned short *)p;
+}
+__device__ __forceinline__ float2 ad_read2(const unsigned char *p) { return *(const float2 *)p; }
+__device__ __forceinline__ int ad_read1(const unsigned char *p) { return *(const int *)p; }
 
-// How a tile's 16 rows of keys and values are dealt to lanes, g = lane / 4, t = lane % 4.  Keys: lane holds of rows g and
-// g + 8 the chunks t, t + 4, ... of KC bytes.  Values: of rows 2t, 2t + 1, 2t + 8, 2t + 9 the chunks g, g + 8, ... of VC bytes.
+// A unit in shared memory: 16 rows of keys, 16 rows of values, RB bytes each, 16-byte chunk c of row r at chunk c ^ swizzle(r).
+// As fragments, g = lane / 4, t = lane % 4: of the keys a lane reads rows g and g + 8, a quarter of each (KN pieces of KC bytes);
+// of the values rows 2t, 2t + 1, 2t + 8, 2t + 9, an eighth of each (VN pieces of VC bytes).
 template <int ST, int HD> struct AdTile {
-    static constexpr int SZ = AdStore<ST>::SIZE;
-    static constexpr int KB = HD * SZ / 4, KC = KB < 16 ? KB : 16, KN = KB / KC; // bytes per lane and row, chunk, chunks
-    static constexpr int VB = HD * SZ / 8, VC = VB < 16 ? VB : 16, VN = VB / VC;
-    static constexpr int VSLOT = VC < 4 ? 4 : VC;                                // 2-byte chunks sit in words of their own
-    static constexpr int K_BYTES = 2 * KN * KC * 32, V_BYTES = 4 * VN * VSLOT * 32;
-    static constexpr int SCALES = K_BYTES + V_BYTES, LIVE = SCALES + (SZ == 1 ? 128 : 0); // then the 32 scales and the number of rows
-    static constexpr int STAGE = LIVE + 16;
-    static constexpr int KE = KC / SZ, VE = VC / SZ;                             // elements per chunk
-    static __device__ __forceinline__ int k_dim(int t, int s) { const int e = 4 * s; return e / KE * (4 * KE) + t * KE + e % KE; } // first of a lane's 4 elements of k-step s
-    static __device__ __forceinline__ int v_dim(int g, int j) { return j / VE * (8 * VE) + g * VE + j % VE; }                      // a lane's j-th element
+    static constexpr int SZ = AdStore<ST>::SIZE, RB = HD * SZ;
+    static constexpr int KB = RB / 4, KC = KB < 16 ? KB : 16, KN = KB / KC;
+    static constexpr int VB = RB / 8, VC = VB < 16 ? VB : 16, VN = VB / VC;
+    static constexpr int U = AdStore<ST>::U, ROWS = 16 * U;
+    static constexpr int K_BYTES = 16 * RB, UNIT = 2 * K_BYTES;
+    static constexpr int SCALES = U * UNIT, LIVE = SCALES + (SZ == 1 ? U * 128 : 0); // per unit 16 + 16 scales, then the number of rows
+    static constexpr int STAGE = LIVE + 16, STAGES = AD_STAGES_DEF;
+    static constexpr int BLOCK_SMEM = AD_WARPS * STAGES * STAGE + (AD_MAX_SEQ + 1) * 8 + AD_MAX_SEQ * 4;
+    static constexpr int FIT = (227 * 1024) / (BLOCK_SMEM + 1024), BLOCKS = FIT < AD_MAXB ? FIT : AD_MAXB; // resident blocks per SM
+    static __device__ __forceinline__ int at(int row, int byte) {
+        const int sw = RB >= 128 ? row & 7 : RB == 64 ? (row >> 1) & 3 : 0;
+        return row * RB + ((byte & ~15) ^ (sw << 4)) + (byte & 15);
+    }
+    static __device__ __forceinline__ int k_byte(int t, int c) { return RB >= 128 ? (2 * t + (c & 1) + 8 * (c >> 1)) * 16 : t * KC; } // lane's piece c of a row of keys
+    static __device__ __forceinline__ int v_byte(int g, int c) { return g * VC + c * 128; }
+    static __device__ __forceinline__ int k_dim(int t, int s) { const int b = 4 * s * SZ; return (k_byte(t, b / KC) + b % KC) / SZ; } // first of a lane's 4 elements of k-step s
+    static __device__ __forceinline__ int v_dim(int g, int j) { const int b = j * SZ; return (v_byte(g, b / VC) + b % VC) / SZ; }     // a lane's j-th element
 };
-template <int ST, int HD> constexpr size_t ad_smem() { return (size_t)AD_WARPS * AD_STAGES * AdTile<ST, HD>::STAGE + (AD_MAX_SEQ + 1) * 8 + AD_MAX_SEQ * 4; }
 
 __device__ __forceinline__ int ad_len(const AdArgs &a, int i, int *status) {
     const int n = a.len[i], slot = a.c.slot ? a.c.slot[i] : a.seq0 + i;
@@ -161,35 +175,51 @@ __device__ __forceinline__ int ad_len(const AdArgs &a, int i, int *status) {
     return n;
 }
 
-// Where in the line of tiles: sequence, (head, chunk) pair within it, tile within the pair
-struct AdCursor {
+// Places in the line of tiles.  Every pair is followed by AD_TURN places without a tile, which stand for what it costs a warp to
+// finish a pair and begin the next: without them, shares full of very short sequences take far longer than the others.
+__device__ __forceinline__ int ad_places(int n_tiles) { return n_tiles > 0 ? n_tiles + AD_TURN : 0; }
+
+// Where in the line: sequence, (head, chunk) pair within it, tile within the pair
+template <int ROWS> struct AdCursor {
     int i, pair, tile, n_tiles, len;
-    __device__ __forceinline__ void enter(const int *s_len, int seq) { i = seq; len = s_len[seq]; n_tiles = (len + 15) >> 4; }
-    __device__ __forceinline__ void seek(const long long *pref, const int *s_len, int n_seq, int pairs, long long at) {
-        int lo = 0, hi = n_seq - 1; // last sequence whose first tile is at or before `at`
+    long long at; // its place
+    __device__ __forceinline__ void enter(const int *s_len, int seq) { i = seq; len = s_len[seq]; n_tiles = (len + ROWS - 1) / ROWS; }
+    // the first tile at or behind place `first`
+    __device__ __forceinline__ void seek(const long long *pref, const int *s_len, int n_seq, int pairs, long long first) {
+        int lo = 0, hi = n_seq - 1; // last sequence that begins at or before it
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
-            if (pref[mid] * pairs <= at) lo = mid; else hi = mid - 1;
+            if (pref[mid] * pairs <= first) lo = mid; else hi = mid - 1;
         }
         enter(s_len, lo);
-        const long long in = at - pref[lo] * pairs;
-        pair = (int)(in / n_tiles);
-        tile = (int)(in - (long long)pair * n_tiles);
+        const int in = (int)(first - pref[lo] * pairs), per = ad_places(n_tiles); // a sequence has fewer than 2^31 places
+        pair = in / per;
+        tile = in - pair * per;
+        at = first;
+        if (tile >= n_tiles) {
+            at += per - tile;
+            next_pair(s_len, n_seq, pairs);
+        }
     }
-    // true: the next tile belongs to another pair
-    __device__ __forceinline__ bool advance(const int *s_len, int n_seq, int pairs) {
-        if (++tile < n_tiles) return false;
+    __device__ __forceinline__ void next_pair(const int *s_len, int n_seq, int pairs) {
         tile = 0;
         if (++pair == pairs) {
             pair = 0;
             do ++i; while (i < n_seq && s_len[i] == 0);
             if (i < n_seq) enter(s_len, i);
         }
+    }
+    // true: the next tile belongs to another pair
+    __device__ __forceinline__ bool advance(const int *s_len, int n_seq, int pairs) {
+        ++at;
+        if (++tile < n_tiles) return false;
+        at += AD_TURN;
+        next_pair(s_len, n_seq, pairs);
         return true;
     }
 };
 
-// share of warp w: tiles [T w / W, T (w + 1) / W)
+// share of warp w: places [T w / W, T (w + 1) / W)
 __device__ __forceinline__ long long ad_share(long long T, int W, int w) { return T * w / W; }
 __device__ __forceinline__ int ad_warps(const AdArgs &a, long long T) {
     const long long w = T / a.min_tiles;
@@ -197,26 +227,27 @@ __device__ __forceinline__ int ad_warps(const AdArgs &a, long long T) {
 }
 
 template <typename RT, int ST, int HD>
-__global__ void __launch_bounds__(AD_THREADS, AdStore<ST>::BLOCKS) k_attn_decode_op(const AdArgs a) {
+__global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_decode_op(const AdArgs a) {
     using TL = AdTile<ST, HD>;
     using BF = std::integral_constant<bool, AdStore<ST>::BF>;
     constexpr bool SCALED = AdStore<ST>::SCALED;
+    constexpr int U = TL::U, STAGES = TL::STAGES;
     constexpr int KS = HD / 16;                       // k-steps of the scores, m-tiles of the output
     constexpr float PUP = AdStore<ST>::BF ? 1.f : 1024.f; // fp16 weights: at most 2^4 * 2 * 2^10
     extern __shared__ __align__(16) unsigned char ad_raw[];
-    long long *s_pref = (long long *)(ad_raw + AD_WARPS * AD_STAGES * TL::STAGE);
+    long long *s_pref = (long long *)(ad_raw + AD_WARPS * STAGES * TL::STAGE);
     int *s_len = (int *)(s_pref + AD_MAX_SEQ + 1);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    // ---- lengths, tiles before each sequence (every block for itself; block 0 leaves them for the joining kernel)
+    // ---- lengths, places before each sequence (every block for itself)
     {
         __shared__ long long s_sum[AD_WARPS];
         long long run = 0;
         for (int base = 0; base < a.n_seq; base += AD_THREADS) {
             const int i = base + tid;
             const int n = i < a.n_seq ? ad_len(a, i, blockIdx.x == 0 ? a.status : nullptr) : 0;
-            const long long mine = (n + 15) >> 4;
+            const long long mine = ad_places((n + TL::ROWS - 1) / TL::ROWS);
             long long incl = mine;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -230,14 +261,10 @@ __global__ void __launch_bounds__(AD_THREADS, AdStore<ST>::BLOCKS) k_attn_decode
             if (i < a.n_seq) {
                 s_len[i] = n;
                 s_pref[i] = before + incl - mine;
-                if (blockIdx.x == 0) a.head[i] = before + incl - mine;
             }
             __syncthreads();
         }
-        if (tid == 0) {
-            s_pref[a.n_seq] = run;
-            if (blockIdx.x == 0) a.head[a.n_seq] = run;
-        }
+        if (tid == 0) s_pref[a.n_seq] = run;
         __syncthreads();
     }
     const int pairs = a.c.n_kv_head * a.chunks;
@@ -245,68 +272,75 @@ __global__ void __launch_bounds__(AD_THREADS, AdStore<ST>::BLOCKS) k_attn_decode
     const int W = ad_warps(a, T), w = blockIdx.x * AD_WARPS + warp;
     if (T == 0 || w >= W) return;
     const long long first = ad_share(T, W, w), last = ad_share(T, W, w + 1);
-    long long left = last - first; // tiles still to compute
-
-    AdCursor cur, nxt; // consumer, producer
+    AdCursor<TL::ROWS> cur, nxt; // consumer, producer
     cur.seek(s_pref, s_len, a.n_seq, pairs, first);
+    if (cur.at >= last) return;
     nxt = cur;
-    long long to_load = left;
     int batch_i = -1, batch_tile = 0, batch_page = -1, page_slot = 0;
-    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(ad_raw) + warp * AD_STAGES * TL::STAGE;
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(ad_raw) + warp * STAGES * TL::STAGE;
     const long long head_rows = (long long)a.c.n_kv_head << a.c.page_shift; // rows of one half of a page
 
     // The next tile into stage `s`.  The lanes hold the page numbers of the next 32 tiles; the rows of a page that does not exist
     // count as behind the end.
     auto load = [&](int s) {
-        if (to_load > 0) {
-            --to_load;
-            if (batch_i != nxt.i || nxt.tile < batch_tile || nxt.tile >= batch_tile + 32) {
+        if (nxt.at < last) {
+            if (batch_i != nxt.i || nxt.tile < batch_tile || nxt.tile == 0 || nxt.tile >= batch_tile + 32 / U) {
+                if (batch_i >= 0 && nxt.tile == 0 && lane < a.hc) { // a new pair's queries, before they are wanted
+                    const int qh = nxt.pair / a.chunks * a.group + nxt.pair % a.chunks * AD_HC + lane;
+                    if (nxt.pair % a.chunks * AD_HC + lane < a.group) {
+                        const unsigned char *q = a.q.data + (nxt.i * a.q.row_stride + qh * a.q.head_stride) * (long long)sizeof(RT);
+#pragma unroll
+                        for (int b = 0; b < HD * (int)sizeof(RT); b += 128) asm volatile("prefetch.global.L1 [%0];" ::"l"(q + b));
+                    }
+                }
                 batch_i = nxt.i;
                 batch_tile = nxt.tile;
                 page_slot = a.c.slot ? a.c.slot[nxt.i] : a.seq0 + nxt.i;
                 batch_page = -1;
-                if (batch_tile + lane < nxt.n_tiles) {
-                    batch_page = __ldg(a.c.table + (long long)page_slot * a.c.table_stride + ((long long)(batch_tile + lane) << 4 >> a.c.page_shift));
+                const int row = (batch_tile * U + lane) << 4;
+                if (row < nxt.len) {
+                    batch_page = __ldg(a.c.table + (long long)page_slot * a.c.table_stride + (row >> a.c.page_shift));
                     if ((unsigned)batch_page >= (unsigned)a.c.n_pages) { op_status(a.status, MDI_STATUS_PAGE); batch_page = -1; }
                 }
             }
-            const int page = __shfl_sync(0xffffffffu, batch_page, nxt.tile - batch_tile);
-            const int row0 = nxt.tile << 4, rows = page < 0 ? 0 : min(16, nxt.len - row0);
             const int h = a.chunks == 1 ? nxt.pair : nxt.pair / a.chunks;
-            const long long kr = (page < 0 ? 0 : ((((long long)page * 2) * a.c.n_kv_head + h) << a.c.page_shift) + (row0 & ((1 << a.c.page_shift) - 1)));
-            const unsigned char *kp = a.c.pool + kr * (HD * TL::SZ), *vp = kp + head_rows * (HD * TL::SZ);
             const uint32_t st = ring + s * TL::STAGE;
 #pragma unroll
-            for (int r = 0; r < 2; ++r)
+            for (int u = 0; u < U; ++u) {
+                const int page = __shfl_sync(0xffffffffu, batch_page, (nxt.tile - batch_tile) * U + u);
+                const int row0 = (nxt.tile * U + u) << 4, rows = page < 0 ? 0 : min(16, nxt.len - row0);
+                const long long kr = page < 0 ? 0 : ((((long long)page * 2) * a.c.n_kv_head + h) << a.c.page_shift) + (row0 & ((1 << a.c.page_shift) - 1));
+                const unsigned char *kp = a.c.pool + kr * TL::RB + lane * 16, *vp = kp + head_rows * TL::RB;
+                const uint32_t sk = st + u * TL::UNIT;
+                constexpr int COPIES = TL::K_BYTES / 512; // of 32 chunks; rows of 16 bytes: half of one
+                if (COPIES > 0 || lane < 16) {
 #pragma unroll
-                for (int c = 0; c < TL::KN; ++c)
-                    ad_copy<TL::KC>(st + ((r * TL::KN + c) * 32 + lane) * TL::KC, kp + (8 * r + g) * (HD * TL::SZ) + (c * 4 + t) * TL::KC, 8 * r + g < rows);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int row = 2 * t + (r & 1) + (r >> 1) * 8;
-#pragma unroll
-                for (int c = 0; c < TL::VN; ++c)
-                    ad_copy<TL::VC>(st + TL::K_BYTES + ((r * TL::VN + c) * 32 + lane) * TL::VSLOT, vp + row * (HD * TL::SZ) + (c * 8 + g) * TL::VC, row < rows);
+                    for (int i = 0; i < (COPIES > 0 ? COPIES : 1); ++i) {
+                        const int row = (i * 512 + lane * 16) / TL::RB, dst = TL::at(row, (i * 512 + lane * 16) % TL::RB);
+                        ad_copy16(sk + dst, kp + i * 512, row < rows);
+                        ad_copy16(sk + TL::K_BYTES + dst, vp + i * 512, row < rows);
+                    }
+                }
+                if (SCALED) { // lanes 0-15 the keys' scales, 16-31 the values'
+                    const int row = lane & 15;
+                    ad_copy4(st + TL::SCALES + u * 128 + lane * 4, a.c.scale + kr + (lane >> 4) * head_rows + row, row < rows);
+                }
+                if (lane == 0) asm volatile("st.shared.s32 [%0], %1;" ::"r"(st + TL::LIVE + u * 4), "r"(rows) : "memory");
             }
-            if (SCALED) { // lanes 0-15 the keys' scales, 16-31 the values'
-                const int row = lane & 15;
-                ad_copy<4>(st + TL::SCALES + lane * 4, (const unsigned char *)(a.c.scale + kr + (lane >> 4) * head_rows + row), row < rows);
-            }
-            if (lane == 0) asm volatile("st.shared.s32 [%0], %1;" ::"r"(st + TL::LIVE), "r"(rows) : "memory");
             nxt.advance(s_len, a.n_seq, pairs);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
 
 #pragma unroll
-    for (int s = 0; s < AD_STAGES - 1; ++s) load(s);
+    for (int s = 0; s < STAGES - 1; ++s) load(s);
 
     uint32_t qa[KS][4];
     float o[KS][4], m = -INFINITY, l = 0.f, q_up = 1.f, v_inv = 1.f;
     int v_exp = 0;
-    bool fresh = true, first_seg = true;
+    bool fresh = true;
     int stage = 0;
-    while (left > 0) {
+    while (cur.at < last) {
         if (fresh) { // a new (sequence, head, chunk): its queries, scaled into log2 units, as fragments
             fresh = false;
             const int h = cur.pair / a.chunks, ch = cur.pair - h * a.chunks;
@@ -331,11 +365,11 @@ __global__ void __launch_bounds__(AD_THREADS, AdStore<ST>::BLOCKS) k_attn_decode
                 }
             q_up = 1.f;
             float q_down = 1.f;
-            if (!AdStore<ST>::BF) { // fp16 planes: the largest element to [1, 2)
+            if (!AdStore<ST>::BF) { // fp16 planes: the largest element to [2^12, 2^13), so that low parts stay normal numbers
                 big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
                 big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
                 if (big != 0 && big < 0x7f800000u) {
-                    const int e = min(max((int)(big >> 23) - 127, -126), 126);
+                    const int e = min(max((int)(big >> 23) - 139, -126), 126);
                     q_up = ad_pow2(e);
                     q_down = ad_pow2(-e);
                 }
@@ -352,47 +386,53 @@ __global__ void __launch_bounds__(AD_THREADS, AdStore<ST>::BLOCKS) k_attn_decode
             v_exp = SCALED ? -126 : 0;
             v_inv = SCALED ? ad_pow2(126) : 1.f;
         }
-        asm volatile("cp.async.wait_group %0;" ::"n"(AD_STAGES - 2) : "memory");
+        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
         __syncwarp();
-        load(stage == 0 ? AD_STAGES - 1 : stage - 1); // the stage that the previous tile used
-        const uint32_t st = ring + stage * TL::STAGE;
-        stage = stage == AD_STAGES - 1 ? 0 : stage + 1;
+        load(stage == 0 ? STAGES - 1 : stage - 1); // the stage that the previous tile used
+        const unsigned char *st = ad_raw + (warp * STAGES + stage) * TL::STAGE;
+        stage = stage == STAGES - 1 ? 0 : stage + 1;
 
-        // ---- scores of 16 rows
-        float s[2][4];
+        // ---- scores: s[2 u + r] are rows 16 u + 8 r + 2t, + 1 for head g (high part of the query, then low part)
+        float s[2 * U][4];
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
+        for (int r = 0; r < 2 * U; ++r)
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[r][e] = 0.f;
-            uint32_t kw[TL::KN][(TL::KC + 3) / 4];
 #pragma unroll
-            for (int c = 0; c < TL::KN; ++c) ad_read<TL::KC>(kw[c], st + ((r * TL::KN + c) * 32 + lane) * TL::KC);
+        for (int c = 0; c < TL::KN; ++c) {
+            constexpr int KPC = TL::KC * 4 / (TL::SZ * 16); // k-steps in a chunk
+            uint32_t kw[2 * U][(TL::KC + 3) / 4];
 #pragma unroll
-            for (int k = 0; k < KS; ++k) {
-                uint32_t b0, b1;
-                if constexpr (TL::SZ == 1) {
-                    const uint32_t x = ad_bias<ST>(kw[k * 4 / TL::KC][k * 4 % TL::KC / 4]);
-                    b0 = ad_wide<ST, 0>(x);
-                    b1 = ad_wide<ST, 1>(x);
-                } else {
-                    b0 = kw[k * 8 / TL::KC][k * 8 % TL::KC / 4];
-                    b1 = kw[k * 8 / TL::KC][k * 8 % TL::KC / 4 + 1];
+            for (int r = 0; r < 2 * U; ++r) ad_read<TL::KC>(kw[r], st + r / 2 * TL::UNIT + r % 2 * 8 * TL::RB + TL::at(g, TL::k_byte(t, c)));
+#pragma unroll
+            for (int k = 0; k < KPC; ++k)
+#pragma unroll
+                for (int r = 0; r < 2 * U; ++r) {
+                    uint32_t b0, b1;
+                    if constexpr (TL::SZ == 1) {
+                        const uint32_t w = ad_bias<ST>(kw[r][k]);
+                        b0 = ad_wide<ST, 0>(w);
+                        b1 = ad_wide<ST, 1>(w);
+                    } else {
+                        b0 = kw[r][2 * k];
+                        b1 = kw[r][2 * k + 1];
+                    }
+                    ad_mma(s[r], qa[c * KPC + k], b0, b1, BF());
                 }
-                ad_mma(s[r], qa[k], b0, b1, BF());
-            }
         }
-        float2 vs[2] = {make_float2(1.f, 1.f), make_float2(1.f, 1.f)};
-        float x[4];
+        float x[4 * U], vs[4 * U]; // scores in log2 units, scales of the values; [4 u + 2 r + b] is row 16 u + 8 r + 2t + b
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            float2 ks = make_float2(q_up, q_up);
+        for (int r = 0; r < 2 * U; ++r) {
+            float2 ks = make_float2(q_up, q_up), v2 = make_float2(1.f, 1.f);
             if (SCALED) {
-                const uint32_t sc = st + TL::SCALES + (8 * r + 2 * t) * 4;
-                asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(ks.x), "=f"(ks.y) : "r"(sc) : "memory");
-                asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(vs[r].x), "=f"(vs[r].y) : "r"(sc + 64) : "memory");
+                const unsigned char *sc = st + TL::SCALES + r / 2 * 128 + (8 * (r % 2) + 2 * t) * 4;
+                ks = ad_read2(sc);
+                v2 = ad_read2(sc + 64);
                 ks.x *= q_up;
                 ks.y *= q_up;
             }
+            vs[2 * r] = v2.x;
+            vs[2 * r + 1] = v2.y;
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 float sum = s[r][b] + s[r][2 + b];
@@ -402,24 +442,25 @@ __global__ void __launch_bounds__(AD_THREADS, AdStore<ST>::BLOCKS) k_attn_decode
             }
         }
         // ---- rows behind the end, or of a page that does not exist
-        {
-            int live;
-            asm volatile("ld.shared.s32 %0, [%1];" : "=r"(live) : "r"(st + TL::LIVE) : "memory");
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int live = ad_read1(st + TL::LIVE + u * 4);
             if (live < 16) {
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    if (8 * r + 2 * t >= live) { x[2 * r] = -INFINITY; vs[r].x = 0.f; }
-                    if (8 * r + 2 * t + 1 >= live) { x[2 * r + 1] = -INFINITY; vs[r].y = 0.f; }
-                }
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+                        if (8 * r + 2 * t + b >= live) { x[4 * u + 2 * r + b] = -INFINITY; vs[4 * u + 2 * r + b] = 0.f; }
             }
         }
         // ---- running maximum; the sums so far follow it only when it rises by more than the slack
-        float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+        float top = x[0], big = vs[0];
+#pragma unroll
+        for (int i = 1; i < 4 * U; ++i) { top = fmaxf(top, x[i]); big = fmaxf(big, vs[i]); }
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
         int e_new = v_exp;
         if (SCALED) {
-            float big = fmaxf(fmaxf(vs[0].x, vs[0].y), fmaxf(vs[1].x, vs[1].y));
             big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
             big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
             e_new = max(v_exp, min((int)(__float_as_uint(big) >> 23) - 127, 126)); // scales are positive
@@ -440,59 +481,61 @@ __global__ void __launch_bounds__(AD_THREADS, AdStore<ST>::BLOCKS) k_attn_decode
             for (int k = 0; k < KS; ++k) { o[k][0] *= f0; o[k][1] *= f1; o[k][2] *= f0; o[k][3] *= f1; }
         }
         const float ref = m == -INFINITY ? 0.f : m;
-        uint32_t ph[2], pl[2];
+        uint32_t ph[2 * U], pl[2 * U];
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            const float p0 = ad_exp2(x[2 * r] - ref), p1 = ad_exp2(x[2 * r + 1] - ref);
+        for (int r = 0; r < 2 * U; ++r) {
+            float p0 = ad_exp2(x[2 * r] - ref), p1 = ad_exp2(x[2 * r + 1] - ref);
             l += p0 + p1;
-            if (SCALED) ad_split(p0 * PUP * (vs[r].x * v_inv), p1 * PUP * (vs[r].y * v_inv), ph[r], pl[r], BF());
-            else ad_split(p0 * PUP, p1 * PUP, ph[r], pl[r], BF());
+            p0 *= PUP;
+            p1 *= PUP;
+            if (SCALED) { p0 *= vs[2 * r] * v_inv; p1 *= vs[2 * r + 1] * v_inv; }
+            ad_split(p0, p1, ph[r], pl[r], BF());
         }
         // ---- values
-        uint32_t vw[4][TL::VN][(TL::VC + 3) / 4];
 #pragma unroll
-        for (int c = 0; c < TL::VN; ++c) {
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) ad_read<TL::VC>(vw[r][c], st + TL::K_BYTES + ((r * TL::VN + c) * 32 + lane) * TL::VSLOT);
+            for (int c = 0; c < TL::VN; ++c) {
+                constexpr int WORDS = (TL::VC + 3) / 4;
+                uint32_t vw[4][WORDS];
 #pragma unroll
-            for (int i = 0; i < (TL::VC + 3) / 4; ++i) {
-                uint32_t av[4];
-                if constexpr (TL::SZ == 1) {
-                    const uint32_t x0 = ad_bias<ST>(vw[0][c][i]), x1 = ad_bias<ST>(vw[1][c][i]), x2 = ad_bias<ST>(vw[2][c][i]), x3 = ad_bias<ST>(vw[3][c][i]);
-                    constexpr int WORDS = (TL::VC + 3) / 4;
-                    const int k = (c * WORDS + i) * 2; // a word holds the elements of two m-tiles
-                    uint32_t y = __byte_perm(x0, x1, 0x5140), z = __byte_perm(x2, x3, 0x5140);
-                    av[0] = ad_wide<ST, 0>(y); av[1] = ad_wide<ST, 1>(y); av[2] = ad_wide<ST, 0>(z); av[3] = ad_wide<ST, 1>(z);
-                    ad_mma(o[k], av, ph[0], ph[1], BF());
-                    ad_mma(o[k], av, pl[0], pl[1], BF());
-                    if constexpr (TL::VC >= 4) {
-                        y = __byte_perm(x0, x1, 0x7362); z = __byte_perm(x2, x3, 0x7362);
+                for (int r = 0; r < 4; ++r) ad_read<TL::VC>(vw[r], st + u * TL::UNIT + TL::K_BYTES + r / 2 * 8 * TL::RB + TL::at(2 * t + r % 2, TL::v_byte(g, c)));
+#pragma unroll
+                for (int i = 0; i < WORDS; ++i) {
+                    if constexpr (TL::SZ == 1) {
+                        const uint32_t x0 = ad_bias<ST>(vw[0][i]), x1 = ad_bias<ST>(vw[1][i]), x2 = ad_bias<ST>(vw[2][i]), x3 = ad_bias<ST>(vw[3][i]);
+                        const int k = (c * WORDS + i) * 2; // a word holds the elements of two m-tiles
+                        uint32_t av[4], aw[4];
+                        uint32_t y = __byte_perm(x0, x1, 0x5140), z = __byte_perm(x2, x3, 0x5140);
                         av[0] = ad_wide<ST, 0>(y); av[1] = ad_wide<ST, 1>(y); av[2] = ad_wide<ST, 0>(z); av[3] = ad_wide<ST, 1>(z);
-                        ad_mma(o[k + 1], av, ph[0], ph[1], BF());
-                        ad_mma(o[k + 1], av, pl[0], pl[1], BF());
+                        ad_mma(o[k], av, ph[2 * u], ph[2 * u + 1], BF());
+                        if constexpr (TL::VC >= 4) {
+                            y = __byte_perm(x0, x1, 0x7362); z = __byte_perm(x2, x3, 0x7362);
+                            aw[0] = ad_wide<ST, 0>(y); aw[1] = ad_wide<ST, 1>(y); aw[2] = ad_wide<ST, 0>(z); aw[3] = ad_wide<ST, 1>(z);
+                            ad_mma(o[k + 1], aw, ph[2 * u], ph[2 * u + 1], BF());
+                        }
+                        ad_mma(o[k], av, pl[2 * u], pl[2 * u + 1], BF());
+                        if constexpr (TL::VC >= 4) ad_mma(o[k + 1], aw, pl[2 * u], pl[2 * u + 1], BF());
+                    } else {
+                        const int k = c * WORDS + i;
+                        uint32_t av[4];
+                        av[0] = __byte_perm(vw[0][i], vw[1][i], 0x5410);
+                        av[1] = __byte_perm(vw[0][i], vw[1][i], 0x7632);
+                        av[2] = __byte_perm(vw[2][i], vw[3][i], 0x5410);
+                        av[3] = __byte_perm(vw[2][i], vw[3][i], 0x7632);
+                        ad_mma(o[k], av, ph[2 * u], ph[2 * u + 1], BF());
+                        ad_mma(o[k], av, pl[2 * u], pl[2 * u + 1], BF());
                     }
-                } else {
-                    const int k = c * (TL::VC / 4) + i;
-                    av[0] = __byte_perm(vw[0][c][i], vw[1][c][i], 0x5410);
-                    av[1] = __byte_perm(vw[0][c][i], vw[1][c][i], 0x7632);
-                    av[2] = __byte_perm(vw[2][c][i], vw[3][c][i], 0x5410);
-                    av[3] = __byte_perm(vw[2][c][i], vw[3][c][i], 0x7632);
-                    ad_mma(o[k], av, ph[0], ph[1], BF());
-                    ad_mma(o[k], av, pl[0], pl[1], BF());
                 }
             }
-        }
         // ---- the end of this pair, or of this warp's share of it
-        --left;
-        const AdCursor was = cur;
+        const AdCursor<TL::ROWS> was = cur;
         const bool turn = cur.advance(s_len, a.n_seq, pairs);
-        if (!turn && left > 0) continue;
+        if (!turn && cur.at < last) continue;
         fresh = true;
         l += __shfl_xor_sync(0xffffffffu, l, 1);
         l += __shfl_xor_sync(0xffffffffu, l, 2);
-        // this warp holds all of the pair if it began at its first tile (its share begins there or it came from another pair)
-        const long long pair_first = s_pref[was.i] * pairs + (long long)was.pair * was.n_tiles;
-        const bool whole = turn && (!first_seg || pair_first >= first);
+        const bool from_start = was.at - was.tile >= first, whole = turn && from_start; // a pair that began in an earlier share has its tile 0 there
         const int h = was.pair / a.chunks, ch = was.pair - h * a.chunks, n_here = min(AD_HC, a.group - ch * AD_HC);
         const float l0 = __shfl_sync(0xffffffffu, l, 8 * t), l1 = __shfl_sync(0xffffffffu, l, 8 * t + 4);
         if (whole) {
@@ -512,7 +555,7 @@ __global__ void __launch_bounds__(AD_THREADS, AdStore<ST>::BLOCKS) k_attn_decode
                 }
             }
         } else {
-            float *p = a.part + ((size_t)w * 2 + (first_seg ? 0 : 1)) * a.hc * (HD + 4);
+            float *p = a.part + ((size_t)w * 2 + (from_start ? 1 : 0)) * a.hc * (HD + 4);
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 if (2 * t + b >= n_here) continue;
@@ -522,71 +565,147 @@ __global__ void __launch_bounds__(AD_THREADS, AdStore<ST>::BLOCKS) k_attn_decode
             }
             if (t == 0 && g < n_here) *(float4 *)(p + g * (HD + 4) + HD) = make_float4(m, l, (float)v_exp, 0.f);
         }
-        first_seg = false;
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
-// Joins what the shares left of a (sequence, query head): grid (n_head, n_seq).  Sequences without rows get zeros.
-template <typename RT, int HD>
-__global__ void __launch_bounds__(AD_MERGE_THREADS) k_attn_decode_join(const AdArgs a, int p_exp) {
-    constexpr int NW = AD_MERGE_THREADS / 32, EPL = HD >= 32 ? HD / 32 : 1;
-    __shared__ float sm_m[NW], sm_l[NW], sm_o[NW][HD];
-    __shared__ int sm_e[NW];
+// Joins what the shares left of a (sequence, query head); NW warps per head, grid (heads / (4 / NW), n_seq).  Sequences without
+// rows get zeros.  What to join follows from the lengths alone, so that is worked out before waiting for the main kernel.
+template <typename RT, int HD, int NW>
+__global__ void __launch_bounds__(AD_JOIN_THREADS) k_attn_decode_join(const AdArgs a, int rows_per_tile, int p_exp) {
+    constexpr int EPL = HD >= 32 ? HD / 32 : 1, AHEAD = 4;
+    __shared__ float sm_m[4], sm_l[4], sm_o[4][HD];
+    __shared__ int sm_e[4];
+    __shared__ long long sm_before[4], sm_total[4];
+    const int i = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int hq = blockIdx.x * (4 / NW) + warp / NW, part_no = warp % NW;
+    long long before = 0, total = 0;
+    for (int j = tid; j < a.n_seq; j += AD_JOIN_THREADS) {
+        const long long n = ad_places((ad_len(a, j, nullptr) + rows_per_tile - 1) / rows_per_tile);
+        total += n;
+        if (j < i) before += n;
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+        before += __shfl_xor_sync(0xffffffffu, before, d);
+        total += __shfl_xor_sync(0xffffffffu, total, d);
+    }
+    if (lane == 0) { sm_before[warp] = before; sm_total[warp] = total; }
+    __syncthreads();
+    before = (sm_before[0] + sm_before[1]) + (sm_before[2] + sm_before[3]);
+    total = (sm_total[0] + sm_total[1]) + (sm_total[2] + sm_total[3]);
+    const int n_tiles = (ad_len(a, i, nullptr) + rows_per_tile - 1) / rows_per_tile;
+    const bool mine = hq < a.n_head;
+    RT *out = (RT *)a.out.data + i * a.out.row_stride + (mine ? hq : 0) * a.out.head_stride;
+    int w0 = 0, w1 = 0, hg = 0;
+    if (n_tiles > 0) {
+        const int pairs = a.c.n_kv_head * a.chunks, h = (mine ? hq : 0) / a.group;
+        hg = (mine ? hq : 0) - h * a.group;
+        const long long T = total * pairs, b0 = before * pairs + (long long)(h * a.chunks + hg / AD_HC) * ad_places(n_tiles), b1 = b0 + n_tiles;
+        const int W = ad_warps(a, T);
+        w0 = (int)(((b0 + 1) * W - 1) / T); // shares that hold the first and the last tile
+        w1 = (int)((b1 * W - 1) / T);
+    }
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int hq = blockIdx.x, i = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    RT *out = (RT *)a.out.data + i * a.out.row_stride + hq * a.out.head_stride;
-    const long long t0 = __ldcg(a.head + i), t1 = __ldcg(a.head + i + 1);
-    const int n_tiles = (int)(t1 - t0);
     if (n_tiles == 0) {
-        if (tid < HD) out[tid] = (RT)0.f;
+        if (mine && part_no == 0)
+            for (int e = lane; e < HD; e += 32) out[e] = (RT)0.f;
         return;
     }
-    const int pairs = a.c.n_kv_head * a.chunks, h = hq / a.group, hg = hq - h * a.group, pair = h * a.chunks + hg / AD_HC;
-    const long long T = __ldcg(a.head + a.n_seq) * pairs, b0 = t0 * pairs + (long long)pair * n_tiles, b1 = b0 + n_tiles;
-    const int W = ad_warps(a, T);
-    const int w0 = (int)(((b0 + 1) * W - 1) / T), w1 = (int)((b1 * W - 1) / T); // shares that hold the first and the last tile
-    if (w0 == w1) return;
+    if (!mine || w0 == w1) return; // the same for all warps of a head
     float m = -INFINITY, l = 0.f, o[EPL];
     int ex = -126;
 #pragma unroll
     for (int e = 0; e < EPL; ++e) o[e] = 0.f;
-    for (int w = w0 + warp; w <= w1; w += NW) {
-        const int slot = w > w0 || ad_share(T, W, w) == b0 ? 0 : 1;
-        const float *p = a.part + (((size_t)w * 2 + slot) * a.hc + hg % AD_HC) * (HD + 4);
-        const float4 st = __ldcg((const float4 *)(p + HD));
-        const float mn = fmaxf(m, st.x), ref = mn == -INFINITY ? 0.f : mn;
-        const int ep = (int)st.z, en = max(ex, ep);
-        const float f_old = ad_exp2(m - ref), f_new = ad_exp2(st.x - ref);
-        const float g_old = f_old * ad_exp2((float)(ex - en)), g_new = f_new * ad_exp2((float)(ep - en));
-        l = l * f_old + st.y * f_new;
+    auto part = [&](int w) { return a.part + (((size_t)w * 2 + (w > w0 ? 0 : 1)) * a.hc + hg % AD_HC) * (HD + 4); }; // of share w
+    auto fetch = [&](float (&y)[EPL], int w) {
+        const float *p = part(min(w, w1));
+#pragma unroll
+        for (int e = 0; e < EPL; ++e)
+            if (HD >= 32 || lane < HD) y[e] = __ldcg(p + lane + 32 * e);
+    };
+    for (int wb = w0 + part_no * 32; wb <= w1; wb += NW * 32) { // a warp takes 32 shares at a time: a lane reads one's statistics ...
+        const int w = wb + lane, n = min(32, w1 - wb + 1);
+        const bool there = w <= w1;
+        const float4 st = there ? __ldcg((const float4 *)(part(w) + HD)) : make_float4(-INFINITY, 0.f, -126.f, 0.f);
+        float y[AHEAD][EPL];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) fetch(y[j], wb + j);
+        float top = st.x, exm = st.z;
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) {
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            exm = fmaxf(exm, __shfl_xor_sync(0xffffffffu, exm, d));
+        }
+        const float mn = fmaxf(m, top), ref = mn == -INFINITY ? 0.f : mn;
+        const int en = max(ex, (int)exm);
+        const float f_old = ad_exp2(m - ref), f_new = there ? ad_exp2(st.x - ref) : 0.f;
+        const float g_old = f_old * ad_exp2((float)(ex - en)), g_new = there ? f_new * ad_exp2(st.z - (float)en) : 0.f;
+        float sum = there ? st.y * f_new : 0.f;
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        l = l * f_old + sum;
         m = mn;
         ex = en;
 #pragma unroll
-        for (int e = 0; e < EPL; ++e)
-            if (HD >= 32 || lane < HD) o[e] = o[e] * g_old + __ldcg(p + lane + 32 * e) * g_new;
+        for (int e = 0; e < EPL; ++e) o[e] *= g_old;
+        for (int j0 = 0; j0 < n; j0 += AHEAD) { // ... and all of them add up the outputs, AHEAD shares' loads in flight
+            float z[AHEAD][EPL];
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) {
+                const float g = __shfl_sync(0xffffffffu, g_new, (j0 + j) & 31);
+#pragma unroll
+                for (int e = 0; e < EPL; ++e) z[j][e] = j0 + j < n ? y[j][e] * g : 0.f;
+            }
+            if (j0 + AHEAD < n) {
+#pragma unroll
+                for (int j = 0; j < AHEAD; ++j) fetch(y[j], wb + j0 + AHEAD + j);
+            }
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j)
+#pragma unroll
+                for (int e = 0; e < EPL; ++e) o[e] += z[j][e];
+        }
     }
-    if (lane == 0) { sm_m[warp] = m; sm_l[warp] = l; sm_e[warp] = ex; }
+    if (NW > 1) { // the head's warps, in their order
+        if (lane == 0) { sm_m[warp] = m; sm_l[warp] = l; sm_e[warp] = ex; }
+#pragma unroll
+        for (int e = 0; e < EPL; ++e)
+            if (HD >= 32 || lane < HD) sm_o[warp][lane + 32 * e] = o[e];
+        __syncthreads();
+        if (warp != 0) return;
+        for (int w = 1; w < NW; ++w) {
+            const float mn = fmaxf(m, sm_m[w]), ref = mn == -INFINITY ? 0.f : mn, f0 = ad_exp2(m - ref), f1 = ad_exp2(sm_m[w] - ref);
+            const int en = max(ex, sm_e[w]);
+            const float g0 = f0 * ad_exp2((float)(ex - en)), g1 = f1 * ad_exp2((float)(sm_e[w] - en));
+            l = l * f0 + sm_l[w] * f1;
+            m = mn;
+            ex = en;
+#pragma unroll
+            for (int e = 0; e < EPL; ++e)
+                if (HD >= 32 || lane < HD) o[e] = o[e] * g0 + sm_o[w][lane + 32 * e] * g1;
+        }
+    }
+    const float down = ad_pow2(max(ex, -116) - p_exp), rest = ad_pow2(min(ex + 116, 0)), inv = 1.f / l;
 #pragma unroll
     for (int e = 0; e < EPL; ++e)
-        if (HD >= 32 || lane < HD) sm_o[warp][lane + 32 * e] = o[e];
-    __syncthreads();
-    if (tid < HD) {
-        float M = -INFINITY, L = 0.f, O = 0.f;
-        int E = -126;
-        for (int w = 0; w < NW; ++w) { M = fmaxf(M, sm_m[w]); E = max(E, sm_e[w]); }
-        const float ref = M == -INFINITY ? 0.f : M;
-        for (int w = 0; w < NW; ++w) {
-            const float f = ad_exp2(sm_m[w] - ref);
-            L += sm_l[w] * f;
-            O += sm_o[w][tid] * f * ad_exp2((float)(sm_e[w] - E));
-        }
-        out[tid] = (RT)(O / L * ad_pow2(max(E, -116) - p_exp) * ad_pow2(min(E + 116, 0)));
-    }
+        if (HD >= 32 || lane < HD) out[lane + 32 * e] = (RT)(o[e] * inv * down * rest);
 }
 
 // ---- host --------------------------------------------------------------------------------------------------------
 struct AdPlan { int chunks, hc, n_warps, min_tiles, blocks; int64_t bytes; };
+
+template <int HD> int ad_blocks_hd(int kv_dtype) {
+    return kv_dtype == MDI_KV_I8 || kv_dtype == MDI_KV_E4M3 ? AdTile<AD_I8, HD>::BLOCKS : AdTile<AD_F16, HD>::BLOCKS;
+}
+int ad_blocks(const mdi_kv_cache *c) {
+    switch (c->head_dim) {
+        case 16: return ad_blocks_hd<16>(c->dtype);
+        case 32: return ad_blocks_hd<32>(c->dtype);
+        case 64: return ad_blocks_hd<64>(c->dtype);
+        default: return ad_blocks_hd<128>(c->dtype);
+    }
+}
 
 AdPlan ad_plan(const mdi_kv_cache *c, int n_seq, int n_head, int max_len) {
     AdPlan p{};
@@ -594,32 +713,36 @@ AdPlan ad_plan(const mdi_kv_cache *c, int n_seq, int n_head, int max_len) {
     p.chunks = (group + AD_HC - 1) / AD_HC;
     p.hc = std::min(group, AD_HC);
     const int64_t cap = (int64_t)c->pages_per_seq * c->page_tokens, len = max_len > 0 ? std::min<int64_t>(max_len, cap) : cap;
-    const int64_t tiles = (int64_t)std::min(n_seq, AD_MAX_SEQ) * c->n_kv_head * p.chunks * ((len + 15) / 16);
+    const int rows = 16 * (op_scaled(c) ? AD_U8 : AD_U16);
+    const int64_t tiles = (int64_t)std::min(n_seq, AD_MAX_SEQ) * c->n_kv_head * p.chunks * ((len + rows - 1) / rows);
     // a share of fewer tiles would leave more bytes of partial results than it reads
     p.min_tiles = 2 + p.hc / 2;
-    const int resident = AD_SM * (op_scaled(c) ? 4 : 2) * AD_WARPS;
+    const int resident = AD_SM * ad_blocks(c) * AD_WARPS;
     p.n_warps = (int)std::max<int64_t>(1, std::min<int64_t>(resident, tiles / p.min_tiles));
     p.blocks = (p.n_warps + AD_WARPS - 1) / AD_WARPS;
-    p.bytes = (AD_MAX_SEQ + 2) * 8 + (int64_t)p.n_warps * 2 * p.hc * (c->head_dim + 4) * 4;
+    p.bytes = (int64_t)p.n_warps * 2 * p.hc * (c->head_dim + 4) * 4;
     return p;
 }
 
 template <typename RT, int ST, int HD> cudaError_t ad_launch(const AdArgs &a, int blocks, cudaStream_t st) {
-    constexpr size_t smem = ad_smem<ST, HD>();
+    constexpr size_t smem = AdTile<ST, HD>::BLOCK_SMEM;
     cudaError_t e = cudaFuncSetAttribute(k_attn_decode_op<RT, ST, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     k_attn_decode_op<RT, ST, HD><<<blocks, AD_THREADS, smem, st>>>(a);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    // many shares per head (few, long sequences): four warps join a head, else one
+    const bool wide = a.n_warps > 64 * a.n_seq * a.c.n_kv_head * a.chunks;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(a.n_head, a.n_seq);
-    cfg.blockDim = dim3(AD_MERGE_THREADS);
+    cfg.gridDim = dim3(wide ? a.n_head : (a.n_head + 3) / 4, a.n_seq);
+    cfg.blockDim = dim3(AD_JOIN_THREADS);
     cfg.stream = st;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, k_attn_decode_join<RT, HD>, a, ST == AD_BF16 ? 0 : 10);
+    const int p_exp = ST == AD_BF16 ? 0 : 10, rows = AdTile<ST, HD>::ROWS;
+    return wide ? cudaLaunchKernelEx(&cfg, k_attn_decode_join<RT, HD, 4>, a, rows, p_exp) : cudaLaunchKernelEx(&cfg, k_attn_decode_join<RT, HD, 1>, a, rows, p_exp);
 }
 template <typename RT, int ST> cudaError_t ad_hd(const AdArgs &a, int blocks, cudaStream_t st) {
     switch (a.c.head_dim) {
@@ -684,8 +807,7 @@ extern "C" int mdi_attn_decode(const mdi_kv_cache *cache, int n_seq, const int32
         a.q.data += i0 * a.q.row_stride * esize;
         a.out.data += i0 * a.out.row_stride * esize;
         a.len = len_dev + i0; a.status = status_dev;
-        a.head = (long long *)workspace_dev;
-        a.part = (float *)((char *)workspace_dev + (AD_MAX_SEQ + 2) * 8);
+        a.part = (float *)workspace_dev;
         a.n_seq = std::min(AD_MAX_SEQ, n_seq - i0); a.seq0 = i0;
         a.n_head = n_head; a.group = n_head / cache->n_kv_head;
         a.chunks = p.chunks; a.hc = p.hc; a.n_warps = p.n_warps; a.min_tiles = p.min_tiles;

@@ -359,11 +359,11 @@ def test_decode_lengths_out_of_range():
     o = torch.full_like(q, 3.0)
     mdi.attn_decode(c.handle, q, o, ints([2 ** 31 - 1, -5, 48]), workspace=ws, status=status)
     assert status.item() == mdi.STATUS_RANGE
-    assert torch.equal(o[0], out[0]) and (o[1] == 0).all() and torch.equal(o[2], out[2])
+    check_decode(c, q, o, [48, 0, 48], [0, 1, 2], F32)         # (how the work is shared out, and with it the bits, may change)
     status.zero_()
     mdi.attn_decode(c.handle, q, o, ints([48, 48, 48]), workspace=ws, slots=ints([0, 77, -1]), status=status)
     assert status.item() == mdi.STATUS_RANGE
-    assert torch.equal(o[0], out[0]) and (o[1:] == 0).all()
+    check_decode(c, q, o, [48, 0, 0], [0, 1, 2], F32)
 
 
 def test_decode_is_reproducible_on_streams_and_in_graphs():
