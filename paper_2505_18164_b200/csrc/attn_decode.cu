@@ -19,9 +19,10 @@
 //    are wide and contiguous; both operands of a product use the same assignment.
 //  * 8-bit elements become fp16 exactly in registers (int8: a byte under the exponent of 1024, minus 1152).  Scales stay
 //    outside of the products: the key's multiplies the score, the value's the weight.
-//  * Rounding: queries and weights are used as two 16-bit planes (high + low, 16 to 22 bits together; queries scaled by a
-//    power of two per head, weights by a power of two that follows the largest value scale seen, so that fp16's range does
-//    not matter); scores, maximum, sums and outputs are fp32.
+//  * Rounding: queries are used as two 16-bit planes (high + low, 16 to 22 bits together; scaled by a power of two per head where
+//    the planes are fp16), weights as two planes, or as one fp16 where the output is 16 bits anyway (half a step of 2^-11 against
+//    the output's own 2^-11 or 2^-8).  Weights refer to a running bound of score and value scale, so that fp16's range does not
+//    matter.  Scores, weights' sums and outputs are fp32.
 #include "ops_common.cuh"
 
 #include <cuda_fp8.h>
@@ -32,7 +33,10 @@
 namespace mdi {
 namespace {
 
-constexpr int AD_WARPS = 4;      // warps per block (they share nothing but the table of lengths)
+#ifndef AD_WARPS_DEF
+#define AD_WARPS_DEF 4
+#endif
+constexpr int AD_WARPS = AD_WARPS_DEF;      // warps per block (they share nothing but the table of lengths)
 constexpr int AD_THREADS = AD_WARPS * 32;
 #ifndef AD_U8
 #define AD_U8 2
@@ -58,7 +62,7 @@ struct AdArgs {
     OpRows q, out;
     const int *len;
     int *status;
-    float *part;      // workspace: [warps][pair from an earlier share | pair that goes on in a later one][hc][HD + 4]: output, maximum, sum, exponent of the weights' scale
+    float *part;      // workspace: [warps][pair from an earlier share | pair that goes on in a later one][hc][HD + 4]: output (not yet divided), what its weights refer to, their sum
     int n_seq, seq0;  // sequences of this launch, first one's number
     int n_head, group, chunks, hc, n_warps, min_tiles;
     float scale_log2e;
@@ -82,6 +86,11 @@ __device__ __forceinline__ void ad_mma(float (&d)[4], const uint32_t (&a)[4], ui
 __device__ __forceinline__ float ad_exp2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float ad_log2(float x) {
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 __device__ __forceinline__ float ad_pow2(int e) { return __uint_as_float((unsigned)(e + 127) << 23); } // -126 <= e <= 127
@@ -233,7 +242,8 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
     constexpr bool SCALED = AdStore<ST>::SCALED;
     constexpr int U = TL::U, STAGES = TL::STAGES;
     constexpr int KS = HD / 16;                       // k-steps of the scores, m-tiles of the output
-    constexpr float PUP = AdStore<ST>::BF ? 1.f : 1024.f; // fp16 weights: at most 2^4 * 2 * 2^10
+    constexpr float UP = AdStore<ST>::BF ? 0.f : 10.f; // weights times value scales stay below 2^(UP + AD_SLACK): inside fp16's range, far from its end
+    constexpr bool PLO = AdStore<ST>::BF || std::is_same<RT, float>::value; // low parts of the weights: see the top of the file
     extern __shared__ __align__(16) unsigned char ad_raw[];
     long long *s_pref = (long long *)(ad_raw + AD_WARPS * STAGES * TL::STAGE);
     int *s_len = (int *)(s_pref + AD_MAX_SEQ + 1);
@@ -305,11 +315,16 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
             }
             const int h = a.chunks == 1 ? nxt.pair : nxt.pair / a.chunks;
             const uint32_t st = ring + s * TL::STAGE;
+            long long kr = 0; // row of the pool
+            int page = -1;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int page = __shfl_sync(0xffffffffu, batch_page, (nxt.tile - batch_tile) * U + u);
-                const int row0 = (nxt.tile * U + u) << 4, rows = page < 0 ? 0 : min(16, nxt.len - row0);
-                const long long kr = page < 0 ? 0 : ((((long long)page * 2) * a.c.n_kv_head + h) << a.c.page_shift) + (row0 & ((1 << a.c.page_shift) - 1));
+                const int row0 = (nxt.tile * U + u) << 4;
+                if (u == 0 || a.c.page_shift == 4) {
+                    page = __shfl_sync(0xffffffffu, batch_page, (nxt.tile - batch_tile) * U + u);
+                    kr = page < 0 ? 0 : ((((long long)page * 2) * a.c.n_kv_head + h) << a.c.page_shift) + (row0 & ((1 << a.c.page_shift) - 1));
+                } else kr += page < 0 ? 0 : 16;
+                const int rows = page < 0 ? 0 : min(16, nxt.len - row0);
                 const unsigned char *kp = a.c.pool + kr * TL::RB + lane * 16, *vp = kp + head_rows * TL::RB;
                 const uint32_t sk = st + u * TL::UNIT;
                 constexpr int COPIES = TL::K_BYTES / 512; // of 32 chunks; rows of 16 bytes: half of one
@@ -336,8 +351,7 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
     for (int s = 0; s < STAGES - 1; ++s) load(s);
 
     uint32_t qa[KS][4];
-    float o[KS][4], m = -INFINITY, l = 0.f, q_up = 1.f, v_inv = 1.f;
-    int v_exp = 0;
+    float o[KS][4], m = -INFINITY, l = 0.f, q_up = 1.f; // m: what weights refer to, 2^(score - m); l: their sum
     bool fresh = true;
     int stage = 0;
     while (cur.at < last) {
@@ -383,8 +397,6 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
             }
             m = -INFINITY;
             l = 0.f;
-            v_exp = SCALED ? -126 : 0;
-            v_inv = SCALED ? ad_pow2(126) : 1.f;
         }
         asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
         __syncwarp();
@@ -420,16 +432,14 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
                     ad_mma(s[r], qa[c * KPC + k], b0, b1, BF());
                 }
         }
-        float x[4 * U], vs[4 * U]; // scores in log2 units, scales of the values; [4 u + 2 r + b] is row 16 u + 8 r + 2t + b
+        float x[4 * U], vs[4 * U]; // scores (times q_up: in log2 units), scales of the values; [4 u + 2 r + b] is row 16 u + 8 r + 2t + b
 #pragma unroll
         for (int r = 0; r < 2 * U; ++r) {
-            float2 ks = make_float2(q_up, q_up), v2 = make_float2(1.f, 1.f);
+            float2 ks = make_float2(1.f, 1.f), v2 = ks;
             if (SCALED) {
                 const unsigned char *sc = st + TL::SCALES + r / 2 * 128 + (8 * (r % 2) + 2 * t) * 4;
                 ks = ad_read2(sc);
                 v2 = ad_read2(sc + 64);
-                ks.x *= q_up;
-                ks.y *= q_up;
             }
             vs[2 * r] = v2.x;
             vs[2 * r + 1] = v2.y;
@@ -438,7 +448,7 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
                 float sum = s[r][b] + s[r][2 + b];
                 // a 16-bit key may be infinite: the low part of the query, of either sign or zero, has no say then
                 if (!SCALED && fabsf(s[r][b]) == INFINITY) sum = s[r][b];
-                x[2 * r + b] = sum * (b ? ks.y : ks.x);
+                x[2 * r + b] = SCALED ? sum * (b ? ks.y : ks.x) : sum;
             }
         }
         // ---- rows behind the end, or of a page that does not exist
@@ -453,29 +463,20 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
                         if (8 * r + 2 * t + b >= live) { x[4 * u + 2 * r + b] = -INFINITY; vs[4 * u + 2 * r + b] = 0.f; }
             }
         }
-        // ---- running maximum; the sums so far follow it only when it rises by more than the slack
+        // ---- what the weights refer to: the largest score, plus the exponent of the largest value scale (weight times scale is
+        // what has to fit fp16; numerator and denominator share the reference), rounded up; it moves only when exceeded by the slack
         float top = x[0], big = vs[0];
 #pragma unroll
         for (int i = 1; i < 4 * U; ++i) { top = fmaxf(top, x[i]); big = fmaxf(big, vs[i]); }
+        top = top * q_up - UP;
+        if (SCALED) top += ad_log2(fminf(fmaxf(big, 0x1p-90f), 0x1p90f));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        int e_new = v_exp;
-        if (SCALED) {
-            big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
-            big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
-            e_new = max(v_exp, min((int)(__float_as_uint(big) >> 23) - 127, 126)); // scales are positive
-        }
         const bool rise = top > m + AD_SLACK || (m == -INFINITY && top > -INFINITY);
-        if (__any_sync(0xffffffffu, rise || e_new != v_exp)) {
-            const float mn = rise ? top : m;
-            float f = rise ? (m == -INFINITY ? 0.f : ad_exp2(m - mn)) : 1.f;
+        if (__any_sync(0xffffffffu, rise)) {
+            const float f = rise ? (m == -INFINITY ? 0.f : ad_exp2(m - top)) : 1.f;
             l *= f;
-            m = mn;
-            if (SCALED) {
-                f *= v_exp - e_new >= -126 ? ad_pow2(v_exp - e_new) : 0.f;
-                v_exp = e_new;
-                v_inv = ad_pow2(-e_new);
-            }
+            if (rise) m = top;
             const float f0 = __shfl_sync(0xffffffffu, f, 8 * t), f1 = __shfl_sync(0xffffffffu, f, 8 * t + 4); // heads 2t, 2t + 1
 #pragma unroll
             for (int k = 0; k < KS; ++k) { o[k][0] *= f0; o[k][1] *= f1; o[k][2] *= f0; o[k][3] *= f1; }
@@ -484,11 +485,9 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
         uint32_t ph[2 * U], pl[2 * U];
 #pragma unroll
         for (int r = 0; r < 2 * U; ++r) {
-            float p0 = ad_exp2(x[2 * r] - ref), p1 = ad_exp2(x[2 * r + 1] - ref);
+            float p0 = ad_exp2(fmaf(x[2 * r], q_up, -ref)), p1 = ad_exp2(fmaf(x[2 * r + 1], q_up, -ref));
             l += p0 + p1;
-            p0 *= PUP;
-            p1 *= PUP;
-            if (SCALED) { p0 *= vs[2 * r] * v_inv; p1 *= vs[2 * r + 1] * v_inv; }
+            if (SCALED) { p0 *= vs[2 * r]; p1 *= vs[2 * r + 1]; }
             ad_split(p0, p1, ph[r], pl[r], BF());
         }
         // ---- values
@@ -514,8 +513,10 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
                             aw[0] = ad_wide<ST, 0>(y); aw[1] = ad_wide<ST, 1>(y); aw[2] = ad_wide<ST, 0>(z); aw[3] = ad_wide<ST, 1>(z);
                             ad_mma(o[k + 1], aw, ph[2 * u], ph[2 * u + 1], BF());
                         }
-                        ad_mma(o[k], av, pl[2 * u], pl[2 * u + 1], BF());
-                        if constexpr (TL::VC >= 4) ad_mma(o[k + 1], aw, pl[2 * u], pl[2 * u + 1], BF());
+                        if constexpr (PLO) {
+                            ad_mma(o[k], av, pl[2 * u], pl[2 * u + 1], BF());
+                            if constexpr (TL::VC >= 4) ad_mma(o[k + 1], aw, pl[2 * u], pl[2 * u + 1], BF());
+                        }
                     } else {
                         const int k = c * WORDS + i;
                         uint32_t av[4];
@@ -524,7 +525,7 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
                         av[2] = __byte_perm(vw[2][i], vw[3][i], 0x5410);
                         av[3] = __byte_perm(vw[2][i], vw[3][i], 0x7632);
                         ad_mma(o[k], av, ph[2 * u], ph[2 * u + 1], BF());
-                        ad_mma(o[k], av, pl[2 * u], pl[2 * u + 1], BF());
+                        if constexpr (PLO) ad_mma(o[k], av, pl[2 * u], pl[2 * u + 1], BF());
                     }
                 }
             }
@@ -539,7 +540,6 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
         const int h = was.pair / a.chunks, ch = was.pair - h * a.chunks, n_here = min(AD_HC, a.group - ch * AD_HC);
         const float l0 = __shfl_sync(0xffffffffu, l, 8 * t), l1 = __shfl_sync(0xffffffffu, l, 8 * t + 4);
         if (whole) {
-            const float down = ad_pow2(max(v_exp, -116) - (AdStore<ST>::BF ? 0 : 10)), rest = ad_pow2(min(v_exp + 116, 0)); // 2^(v_exp - 10) in two factors
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 if (2 * t + b >= n_here) continue;
@@ -547,7 +547,7 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
                 RT *out = (RT *)a.out.data + was.i * a.out.row_stride + (h * a.group + ch * AD_HC + 2 * t + b) * a.out.head_stride;
 #pragma unroll
                 for (int k = 0; k < KS; ++k) {
-                    const float y0 = o[k][b] * inv * down * rest, y1 = o[k][2 + b] * inv * down * rest;
+                    const float y0 = o[k][b] * inv, y1 = o[k][2 + b] * inv;
                     const int d = TL::v_dim(g, 2 * k);
                     if constexpr (std::is_same<RT, float>::value) *(float2 *)(out + d) = make_float2(y0, y1);
                     else if constexpr (std::is_same<RT, __half>::value) *(__half2 *)(out + d) = __floats2half2_rn(y0, y1);
@@ -563,7 +563,7 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
 #pragma unroll
                 for (int k = 0; k < KS; ++k) *(float2 *)(ph_ + TL::v_dim(g, 2 * k)) = make_float2(o[k][b], o[k][2 + b]);
             }
-            if (t == 0 && g < n_here) *(float4 *)(p + g * (HD + 4) + HD) = make_float4(m, l, (float)v_exp, 0.f);
+            if (t == 0 && g < n_here) *(float4 *)(p + g * (HD + 4) + HD) = make_float4(m, l, 0.f, 0.f);
         }
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
@@ -572,10 +572,9 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
 // Joins what the shares left of a (sequence, query head); NW warps per head, grid (heads / (4 / NW), n_seq).  Sequences without
 // rows get zeros.  What to join follows from the lengths alone, so that is worked out before waiting for the main kernel.
 template <typename RT, int HD, int NW>
-__global__ void __launch_bounds__(AD_JOIN_THREADS) k_attn_decode_join(const AdArgs a, int rows_per_tile, int p_exp) {
-    constexpr int EPL = HD >= 32 ? HD / 32 : 1, AHEAD = 4;
+__global__ void __launch_bounds__(AD_JOIN_THREADS) k_attn_decode_join(const AdArgs a, int rows_per_tile) {
+    constexpr int EPL = HD >= 32 ? HD / 32 : 1, AHEAD = 8;
     __shared__ float sm_m[4], sm_l[4], sm_o[4][HD];
-    __shared__ int sm_e[4];
     __shared__ long long sm_before[4], sm_total[4];
     const int i = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int hq = blockIdx.x * (4 / NW) + warp / NW, part_no = warp % NW;
@@ -614,41 +613,35 @@ __global__ void __launch_bounds__(AD_JOIN_THREADS) k_attn_decode_join(const AdAr
     }
     if (!mine || w0 == w1) return; // the same for all warps of a head
     float m = -INFINITY, l = 0.f, o[EPL];
-    int ex = -126;
 #pragma unroll
     for (int e = 0; e < EPL; ++e) o[e] = 0.f;
+    const int per = (w1 - w0 + NW) / NW, my0 = w0 + part_no * per, my1 = min(w1, my0 + per - 1); // this warp's shares
     auto part = [&](int w) { return a.part + (((size_t)w * 2 + (w > w0 ? 0 : 1)) * a.hc + hg % AD_HC) * (HD + 4); }; // of share w
     auto fetch = [&](float (&y)[EPL], int w) {
-        const float *p = part(min(w, w1));
+        const float *p = part(min(w, my1));
 #pragma unroll
         for (int e = 0; e < EPL; ++e)
             if (HD >= 32 || lane < HD) y[e] = __ldcg(p + lane + 32 * e);
     };
-    for (int wb = w0 + part_no * 32; wb <= w1; wb += NW * 32) { // a warp takes 32 shares at a time: a lane reads one's statistics ...
-        const int w = wb + lane, n = min(32, w1 - wb + 1);
-        const bool there = w <= w1;
-        const float4 st = there ? __ldcg((const float4 *)(part(w) + HD)) : make_float4(-INFINITY, 0.f, -126.f, 0.f);
+    for (int wb = my0; wb <= my1; wb += 32) { // 32 shares at a time: a lane reads one's statistics ...
+        const int w = wb + lane, n = min(32, my1 - wb + 1);
+        const bool there = w <= my1;
+        const float2 st = there ? __ldcg((const float2 *)(part(w) + HD)) : make_float2(-INFINITY, 0.f);
         float y[AHEAD][EPL];
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) fetch(y[j], wb + j);
-        float top = st.x, exm = st.z;
+        float top = st.x;
 #pragma unroll
-        for (int d = 16; d > 0; d >>= 1) {
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-            exm = fmaxf(exm, __shfl_xor_sync(0xffffffffu, exm, d));
-        }
+        for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
         const float mn = fmaxf(m, top), ref = mn == -INFINITY ? 0.f : mn;
-        const int en = max(ex, (int)exm);
-        const float f_old = ad_exp2(m - ref), f_new = there ? ad_exp2(st.x - ref) : 0.f;
-        const float g_old = f_old * ad_exp2((float)(ex - en)), g_new = there ? f_new * ad_exp2(st.z - (float)en) : 0.f;
-        float sum = there ? st.y * f_new : 0.f;
+        const float f_old = ad_exp2(m - ref), g_new = there ? ad_exp2(st.x - ref) : 0.f;
+        float sum = there ? st.y * g_new : 0.f;
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
         l = l * f_old + sum;
         m = mn;
-        ex = en;
 #pragma unroll
-        for (int e = 0; e < EPL; ++e) o[e] *= g_old;
+        for (int e = 0; e < EPL; ++e) o[e] *= f_old;
         for (int j0 = 0; j0 < n; j0 += AHEAD) { // ... and all of them add up the outputs, AHEAD shares' loads in flight
             float z[AHEAD][EPL];
 #pragma unroll
@@ -668,7 +661,7 @@ __global__ void __launch_bounds__(AD_JOIN_THREADS) k_attn_decode_join(const AdAr
         }
     }
     if (NW > 1) { // the head's warps, in their order
-        if (lane == 0) { sm_m[warp] = m; sm_l[warp] = l; sm_e[warp] = ex; }
+        if (lane == 0) { sm_m[warp] = m; sm_l[warp] = l; }
 #pragma unroll
         for (int e = 0; e < EPL; ++e)
             if (HD >= 32 || lane < HD) sm_o[warp][lane + 32 * e] = o[e];
@@ -676,20 +669,17 @@ __global__ void __launch_bounds__(AD_JOIN_THREADS) k_attn_decode_join(const AdAr
         if (warp != 0) return;
         for (int w = 1; w < NW; ++w) {
             const float mn = fmaxf(m, sm_m[w]), ref = mn == -INFINITY ? 0.f : mn, f0 = ad_exp2(m - ref), f1 = ad_exp2(sm_m[w] - ref);
-            const int en = max(ex, sm_e[w]);
-            const float g0 = f0 * ad_exp2((float)(ex - en)), g1 = f1 * ad_exp2((float)(sm_e[w] - en));
             l = l * f0 + sm_l[w] * f1;
             m = mn;
-            ex = en;
 #pragma unroll
             for (int e = 0; e < EPL; ++e)
-                if (HD >= 32 || lane < HD) o[e] = o[e] * g0 + sm_o[w][lane + 32 * e] * g1;
+                if (HD >= 32 || lane < HD) o[e] = o[e] * f0 + sm_o[w][lane + 32 * e] * f1;
         }
     }
-    const float down = ad_pow2(max(ex, -116) - p_exp), rest = ad_pow2(min(ex + 116, 0)), inv = 1.f / l;
+    const float inv = 1.f / l;
 #pragma unroll
     for (int e = 0; e < EPL; ++e)
-        if (HD >= 32 || lane < HD) out[lane + 32 * e] = (RT)(o[e] * inv * down * rest);
+        if (HD >= 32 || lane < HD) out[lane + 32 * e] = (RT)(o[e] * inv);
 }
 
 // ---- host --------------------------------------------------------------------------------------------------------
@@ -731,7 +721,7 @@ template <typename RT, int ST, int HD> cudaError_t ad_launch(const AdArgs &a, in
     k_attn_decode_op<RT, ST, HD><<<blocks, AD_THREADS, smem, st>>>(a);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
     // many shares per head (few, long sequences): four warps join a head, else one
-    const bool wide = a.n_warps > 64 * a.n_seq * a.c.n_kv_head * a.chunks;
+    const bool wide = a.n_warps > 8 * a.n_seq * a.c.n_kv_head * a.chunks;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(wide ? a.n_head : (a.n_head + 3) / 4, a.n_seq);
     cfg.blockDim = dim3(AD_JOIN_THREADS);
@@ -741,8 +731,8 @@ template <typename RT, int ST, int HD> cudaError_t ad_launch(const AdArgs &a, in
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    const int p_exp = ST == AD_BF16 ? 0 : 10, rows = AdTile<ST, HD>::ROWS;
-    return wide ? cudaLaunchKernelEx(&cfg, k_attn_decode_join<RT, HD, 4>, a, rows, p_exp) : cudaLaunchKernelEx(&cfg, k_attn_decode_join<RT, HD, 1>, a, rows, p_exp);
+    const int rows = AdTile<ST, HD>::ROWS;
+    return wide ? cudaLaunchKernelEx(&cfg, k_attn_decode_join<RT, HD, 4>, a, rows) : cudaLaunchKernelEx(&cfg, k_attn_decode_join<RT, HD, 1>, a, rows);
 }
 template <typename RT, int ST> cudaError_t ad_hd(const AdArgs &a, int blocks, cudaStream_t st) {
     switch (a.c.head_dim) {
