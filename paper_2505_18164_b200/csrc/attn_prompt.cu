@@ -5,13 +5,17 @@
 // exponentials (one per query, head and key, 16 a clock and SM).
 //
 // One block takes 256 query rows of one head (two sub-tiles of 128) and walks the keys its rows see in tiles of 128, once:
-//   warp 8      requests the tiles by TMA (128-byte swizzle, no multicast): queries once, then keys and values through one ring;
-//   warp 9      issues tcgen05.mma: scores S = Q K^T (128 x 128) and outputs O += P V, accumulators in tensor memory.  The
-//               sub-tiles alternate, so that one's products run while the other's softmax does;
-//   warps 0-3, 4-7  softmax of sub-tile 0 and 1, one row per thread: scores from tensor memory, running maximum and sum in fp32,
-//               weights rounded to the type of V back into the tensor memory of the scores (an A operand is read from there).
-//               What has been summed in O is rescaled only when a row's maximum rises by more than 2^8 (weights stay below
-//               that; sums are fp32), so that the outputs hardly ever leave tensor memory on the way.
+//   warp 16     requests the tiles by TMA (128-byte swizzle, no multicast): queries once, then keys and values through one ring;
+//   warp 17     issues tcgen05.mma: scores S = Q K^T (128 x 128) and outputs O += P V, accumulators in tensor memory, in the fixed
+//               order P0 V, next S0, P1 V, next S1: one sub-tile's products run while the other's softmax does.  (With a warp for each
+//               sub-tile the products interleave, both softmaxes start together and wait for the exponential unit together: a tile
+//               took 5500 clocks instead of the [[CLK]].)
+//   warps 0-7, 8-15  softmax of sub-tile 0 and 1.  A row belongs to two threads, 64 keys of a tile each (one thread per row left the
+//               schedulers with two warps each and waited for latencies: 1.7x the time): scores from tensor memory, maximum and sum
+//               in fp32, weights rounded to the type of V back into the tensor memory of the scores (an A operand is read from
+//               there) in two steps, so that the product of the first half runs while the second is computed.  Weights refer to a
+//               maximum that both threads of a row hold; it moves, and what has been summed in O is rescaled, only when a score exceeds it by 2^8
+//               (weights stay below that; sums are fp32), so the two hardly ever talk and O hardly ever leaves tensor memory.
 // The scores' accumulator ready implies that the sub-tile's previous output product is complete (both are committed in order),
 // which is what makes the rescaling safe.
 //
@@ -30,15 +34,19 @@
 namespace mdi {
 namespace {
 
+#ifndef AP_POLY
+#define AP_POLY 6
+#endif
 constexpr int AP_ROWS = 128;              // rows of a sub-tile, keys of a tile
-constexpr int AP_THREADS = 320;
+constexpr int AP_THREADS = 640;
+constexpr int AP_SORT = 64;               // up to this many sequences their tiles are taken in order of the keys they see
 constexpr unsigned long long AP_WAIT_NS = 2000000000ull;
 
 struct ApArgs {
     OpRows v, out;
     const int *q_start, *k_start;
     int *status;
-    int n_seq, n_q, n_k, group, hd;
+    int n_seq, n_q, n_k, n_head, group, hd;
     int q_swap, k_swap, v_swap; // the tensor map has (element, row, head) instead of (element, head, row)
     float scale_log2e;
 };
@@ -47,16 +55,17 @@ template <int HDP> struct ApLayout {
     static constexpr int TILE = AP_ROWS * HDP * 2;
     static constexpr int STAGES = HDP == 128 ? 5 : 8;
     static constexpr int Q = 0, RING = 2 * TILE, BARS = RING + STAGES * TILE;
-    static constexpr int SMEM = BARS + 256 + 1024; // barriers, alignment slack
+    static constexpr int SMEM = BARS + 2560; // barriers and what threads tell each other
 };
 
 struct ApShared { // behind the ring
-    unsigned long long qfull, full[8], empty[8], sready[2], pready[2], odone[2], drain;
+    unsigned long long qfull, full[8], empty[8], sready[2], pready[4], odone[2], drain;
     unsigned tmem;
     int abort, poison;
-    int seq, tile, q0, nq, k0, nk; // this block's sequence
+    float row[2][2][AP_ROWS];      // [sub-tile][half][row]: what the two threads of a row tell each other
+    int tile, q0, nq, k0, nk; // this block's tile (negative: none) and its sequence
 };
-static_assert(sizeof(ApShared) <= 256, "ApShared");
+static_assert(sizeof(ApShared) <= 2560, "ApShared");
 
 __device__ __forceinline__ void ap_init(uint32_t bar, int n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(n) : "memory"); }
 __device__ __forceinline__ void ap_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
@@ -66,12 +75,13 @@ __device__ __forceinline__ void ap_expect(uint32_t bar, uint32_t bytes) {
 // false: the wait gave up, or another one of the block did
 __device__ __noinline__ bool ap_wait_slow(uint32_t bar, uint32_t parity, int *abort, int *status) {
     const unsigned long long t0 = tg_now();
-    for (unsigned it = 0;; ++it) {
-        if (tg_try_wait(bar, parity)) return true;
-        if ((it & 15u) == 15u) {
-            if (*(volatile int *)abort) return false;
-            if (tg_now() - t0 > AP_WAIT_NS) break;
-        }
+    for (;;) {
+        uint32_t done; // the thread may sleep for up to 20 us: polling takes issue slots from the softmax
+        asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n selp.u32 %0, 1, 0, p;\n}\n"
+                     : "=r"(done) : "r"(bar), "r"(parity), "r"(20000) : "memory");
+        if (done) return true;
+        if (*(volatile int *)abort) return false;
+        if (tg_now() - t0 > AP_WAIT_NS) break;
     }
     *(volatile int *)abort = 1;
     op_status(status, MDI_STATUS_TIMEOUT);
@@ -89,20 +99,31 @@ template <int HDP> __device__ __forceinline__ void ap_load(uint32_t dst, const C
 #pragma unroll
     for (int b = 0; b < HDP / 64; ++b) ap_tma(dst + b * (AP_ROWS * 128), map, b * 64, swapped ? row : head, swapped ? head : row, bar);
 }
-// Descriptor of an operand whose rows run along the reduction (values: [key][64 elements of head_dim], 128 bytes a key, swizzled):
-// 8 keys = 1024 bytes, the next 64 elements of head_dim one box further.
+// ---- issued by a whole warp in step (one elected lane): the compiler can then keep descriptors in uniform registers; with one
+// thread of a diverged warp issuing, moving them there took longer than the products (90 instead of 64 clocks each)
+__device__ __forceinline__ bool ap_wait_warp(uint32_t bar, uint32_t parity, int *abort, int *status) {
+    bool ok = tg_try_wait(bar, parity);
+    if (!__all_sync(0xffffffffu, ok)) ok = ok || ap_wait_slow(bar, parity, abort, status);
+    return __all_sync(0xffffffffu, ok);
+}
+// Shared-memory descriptors.  Queries and keys: rows of 128 bytes along head_dim, 128-byte swizzle, 8 rows = 1024 bytes.  Values: the
+// rows run along the reduction (keys), the next 64 elements of head_dim are one box further.
+__device__ __forceinline__ uint64_t ap_desc(uint32_t addr) {
+    return ((uint64_t)(1u << 14 | 1024 >> 4 | 2u << 29) << 32) | 1u << 16 | addr >> 4; // version 1, swizzle 2; addr < 2^18
+}
 __device__ __forceinline__ uint64_t ap_desc_mn(uint32_t addr) {
-    uint64_t d = 0;
-    d |= (uint64_t)((addr & 0x3FFFF) >> 4);
-    d |= (uint64_t)((AP_ROWS * 128) >> 4) << 16;
-    d |= (uint64_t)(1024 >> 4) << 32;
-    d |= (uint64_t)1 << 46;
-    d |= (uint64_t)2 << 61;
-    return d;
+    return ((uint64_t)(1u << 14 | 1024 >> 4 | 2u << 29) << 32) | (uint32_t)((AP_ROWS * 128) >> 4) << 16 | addr >> 4;
+}
+__device__ __forceinline__ void ap_mma_ss(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n .reg .pred p, e;\n elect.sync _|e, 0xffffffff;\n setp.ne.b32 p, %4, 0;\n @e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
+                 ::"r"(d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
 }
 __device__ __forceinline__ void ap_mma_ts(uint32_t d, uint32_t a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
+    asm volatile("{\n .reg .pred p, e;\n elect.sync _|e, 0xffffffff;\n setp.ne.b32 p, %4, 0;\n @e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
                  ::"r"(d), "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void ap_commit(uint32_t bar) {
+    asm volatile("{\n .reg .pred e;\n elect.sync _|e, 0xffffffff;\n @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(bar) : "memory");
 }
 #define AP_R32(r, o) "=r"(r[o]), "=r"(r[o + 1]), "=r"(r[o + 2]), "=r"(r[o + 3]), "=r"(r[o + 4]), "=r"(r[o + 5]), "=r"(r[o + 6]), "=r"(r[o + 7]), \
     "=r"(r[o + 8]), "=r"(r[o + 9]), "=r"(r[o + 10]), "=r"(r[o + 11]), "=r"(r[o + 12]), "=r"(r[o + 13]), "=r"(r[o + 14]), "=r"(r[o + 15]), \
@@ -121,12 +142,55 @@ template <int N> __device__ __forceinline__ void ap_st32(uint32_t addr, const ui
     asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
                  "%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(addr), AP_W32(r, o) : "memory");
 }
+__device__ __forceinline__ void ap_ld16(uint32_t (&r)[16], uint32_t addr) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+                   "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(addr) : "memory");
+}
+template <int N> __device__ __forceinline__ void ap_st16(uint32_t addr, const uint32_t (&r)[N], int o) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                 ::"r"(addr), "r"(r[o]), "r"(r[o + 1]), "r"(r[o + 2]), "r"(r[o + 3]), "r"(r[o + 4]), "r"(r[o + 5]), "r"(r[o + 6]), "r"(r[o + 7]),
+                 "r"(r[o + 8]), "r"(r[o + 9]), "r"(r[o + 10]), "r"(r[o + 11]), "r"(r[o + 12]), "r"(r[o + 13]), "r"(r[o + 14]), "r"(r[o + 15]) : "memory");
+}
 __device__ __forceinline__ void ap_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void ap_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ float ap_exp2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+// pairs of fp32 in one instruction
+typedef unsigned long long ap_f2;
+__device__ __forceinline__ ap_f2 ap_pair(float a, float b) { ap_f2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void ap_unpair(ap_f2 p, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p)); }
+__device__ __forceinline__ ap_f2 ap_fma2(ap_f2 a, ap_f2 b, ap_f2 c) { ap_f2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ ap_f2 ap_add2(ap_f2 a, ap_f2 b) { ap_f2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ float ap_max_nan(float a, float b, float c) { float r; asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; } // NaN if one is
+
+// 2^x on the multiply-add pipe, for x in [-125, 2^22) (below -125: 2^-125): x = n + f with f in [-1/2, 1/2], a polynomial in f
+// that is minimax in the relative error (degree 3: 7.5e-5, a 26th of bf16's half step; degree 4: 2.7e-6, for fp16; fitted by the
+// exchange algorithm), n added to its exponent.
+template <typename T> __device__ __forceinline__ void ap_exp2_poly(ap_f2 x, float &p0, float &p1) {
+    float x0, x1, t0, t1;
+    ap_unpair(x, x0, x1);
+    x = ap_pair(fmaxf(x0, -125.f), fmaxf(x1, -125.f));
+    const ap_f2 magic = ap_pair(12582912.f, 12582912.f), unmagic = ap_pair(-12582912.f, -12582912.f), minus = ap_pair(-1.f, -1.f);
+    const ap_f2 t = ap_add2(x, magic), f = ap_fma2(ap_add2(t, unmagic), minus, x);
+    ap_f2 y;
+    if constexpr (std::is_same<T, __half>::value) {
+        y = ap_fma2(f, ap_pair(0.0095701022f, 0.0095701022f), ap_pair(0.0559178591f, 0.0559178591f));
+        y = ap_fma2(y, f, ap_pair(0.2402474433f, 0.2402474433f));
+        y = ap_fma2(y, f, ap_pair(0.6931217909f, 0.6931217909f));
+        y = ap_fma2(y, f, ap_pair(0.9999992847f, 0.9999992847f));
+    } else {
+        y = ap_fma2(f, ap_pair(0.0551716685f, 0.0551716685f), ap_pair(0.2426111251f, 0.2426111251f));
+        y = ap_fma2(y, f, ap_pair(0.6932609677f, 0.6932609677f));
+        y = ap_fma2(y, f, ap_pair(0.9999280572f, 0.9999280572f));
+    }
+    ap_unpair(t, t0, t1);
+    ap_unpair(y, p0, p1);
+    p0 = __uint_as_float(__float_as_uint(p0) + (__float_as_uint(t0) << 23));
+    p1 = __uint_as_float(__float_as_uint(p1) + (__float_as_uint(t1) << 23));
 }
 
 template <typename T> __device__ __forceinline__ uint32_t ap_pack(float x, float y);
@@ -137,80 +201,102 @@ template <typename T> __device__ __forceinline__ uint32_t ap_nonfinite(uint32_t 
     return std::is_same<T, __half>::value ? ((w & 0x7c007c00u) + 0x04000400u) & 0x80008000u : ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
 }
 
-// Sequence and 256-row tile of the block: the tiles of all sequences end to end, the last one first (it sees the most keys).
-// One warp.  A sequence whose offsets do not fit has no tiles.
+// Sequence and 256-row tile of the block, x-th in the order in which tiles are taken.  One warp.  A sequence whose offsets do not
+// fit has no tiles.  Tiles that see the most keys come first, so that no long one is left to run alone at the end: over all
+// sequences where there are at most AP_SORT (found by bisection on the number of key tiles), else sequence by sequence.
+struct ApSeq { int q0, nq, k0, nk, tiles; };
+__device__ __forceinline__ ApSeq ap_seq(const ApArgs &a, int i, bool tell) {
+    ApSeq s{};
+    if (i >= a.n_seq) return s;
+    const int q0 = a.q_start[i], q1 = a.q_start[i + 1], k0 = a.k_start[i], k1 = a.k_start[i + 1];
+    if (q0 < 0 || q1 < q0 || q1 > a.n_q || k0 < 0 || k1 < k0 || k1 > a.n_k) {
+        if (tell) op_status(a.status, MDI_STATUS_RANGE);
+        return s;
+    }
+    s.q0 = q0; s.nq = q1 - q0; s.k0 = k0; s.nk = k1 - k0;
+    s.tiles = (s.nq + 2 * AP_ROWS - 1) / (2 * AP_ROWS);
+    return s;
+}
+// tiles of the sequence that see at least `level` key tiles (the last ones; tile t sees the keys up to off + 256 (t + 1))
+__device__ __forceinline__ int ap_at_least(const ApSeq &s, int level) {
+    const int keys = (level - 1) * AP_ROWS; // more than this many
+    if (level <= 0) return s.tiles;
+    if (s.nk <= keys || s.tiles == 0) return 0;
+    const int first = keys - (s.nk - s.nq) < 0 ? 0 : (keys - (s.nk - s.nq)) / (2 * AP_ROWS);
+    return s.tiles - min(first, s.tiles - 1);
+}
+__device__ __forceinline__ int ap_sum(int n) { return __reduce_add_sync(0xffffffffu, n); }
+__device__ __forceinline__ int ap_scan(int n, int lane) { // sum over the lanes up to this one
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, n, o);
+        if (lane >= o) n += up;
+    }
+    return n;
+}
+__device__ __forceinline__ void ap_found(ApShared *sh, const ApSeq &s, int tile) {
+    sh->tile = tile; sh->q0 = s.q0; sh->nq = s.nq; sh->k0 = s.k0; sh->nk = s.nk;
+}
 __device__ __forceinline__ void ap_find_tile(const ApArgs &a, int x, int lane, ApShared *sh) {
-    auto tiles_of = [&](int i, bool tell) {
-        if (i >= a.n_seq) return 0;
-        const int q0 = a.q_start[i], q1 = a.q_start[i + 1], k0 = a.k_start[i], k1 = a.k_start[i + 1];
-        const bool bad = q0 < 0 || q1 < q0 || q1 > a.n_q || k0 < 0 || k1 < k0 || k1 > a.n_k;
-        if (bad && tell) op_status(a.status, MDI_STATUS_RANGE);
-        return bad ? 0 : (q1 - q0 + 2 * AP_ROWS - 1) / (2 * AP_ROWS);
-    };
-    const bool tell = blockIdx.x == 0 && blockIdx.y == 0;
-    long long total = 0;
-    for (int b = 0; b < a.n_seq; b += 32) {
-        int n = tiles_of(b + lane, tell);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
-        total += n;
-    }
-    if (lane == 0) sh->seq = -1;
+    const bool tell = blockIdx.x == 0;
+    if (lane == 0) sh->tile = -1;
     __syncwarp();
-    const long long at = total - 1 - x;
-    if (at < 0) return;
-    long long before = 0;
-    for (int b = 0; b < a.n_seq && before <= at; b += 32) {
-        const int n = tiles_of(b + lane, false);
-        int incl = n;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int up = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += up;
+    if (a.n_seq <= AP_SORT) {
+        const ApSeq s0 = ap_seq(a, lane, tell), s1 = ap_seq(a, lane + 32, tell);
+        if (x >= ap_sum(s0.tiles + s1.tiles)) return;
+        int lo = 0, hi = (__reduce_max_sync(0xffffffffu, max(s0.nk, s1.nk)) + AP_ROWS - 1) / AP_ROWS; // the largest level with more than x tiles at or above it
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (ap_sum(ap_at_least(s0, mid) + ap_at_least(s1, mid)) > x) lo = mid; else hi = mid - 1;
         }
-        const long long lo = before + incl - n;
-        if (n > 0 && lo <= at && at < lo + n) {
-            const int i = b + lane;
-            sh->seq = i;
-            sh->tile = (int)(at - lo);
-            sh->q0 = a.q_start[i];
-            sh->nq = a.q_start[i + 1] - a.q_start[i];
-            sh->k0 = a.k_start[i];
-            sh->nk = a.k_start[i + 1] - a.k_start[i];
+        const int a0 = ap_at_least(s0, lo), a1 = ap_at_least(s1, lo), n0 = a0 - ap_at_least(s0, lo + 1), n1 = a1 - ap_at_least(s1, lo + 1);
+        const int rank = x - (ap_sum(a0 + a1) - ap_sum(n0 + n1)); // among the tiles of exactly this level
+        const int before = ap_scan(n0 + n1, lane) - n0 - n1;
+        if (rank >= before && rank < before + n0) ap_found(sh, s0, s0.tiles - a0 + rank - before);
+        else if (rank >= before + n0 && rank < before + n0 + n1) ap_found(sh, s1, s1.tiles - a1 + rank - before - n0);
+    } else {
+        long long total = 0;
+        for (int b = 0; b < a.n_seq; b += 32) total += ap_sum(ap_seq(a, b + lane, tell).tiles);
+        const long long at = total - 1 - x;
+        long long before = 0;
+        for (int b = 0; b < a.n_seq && before <= at; b += 32) {
+            const ApSeq s = ap_seq(a, b + lane, false);
+            const int incl = ap_scan(s.tiles, lane);
+            const long long lo = before + incl - s.tiles;
+            if (lo <= at && at < lo + s.tiles) ap_found(sh, s, (int)(at - lo));
+            before += __shfl_sync(0xffffffffu, incl, 31);
         }
-        before += __shfl_sync(0xffffffffu, incl, 31);
     }
-    __syncwarp();
 }
 
-// grid (tiles, n_head)
+// grid: tiles x heads, the heads of a tile next to each other
 template <typename T, int HDP>
 __global__ void __launch_bounds__(AP_THREADS, 1)
 k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const ApArgs a) {
     using L = ApLayout<HDP>;
     constexpr bool BF = std::is_same<T, __nv_bfloat16>::value;
     constexpr int NST = L::STAGES;
-    extern __shared__ unsigned char ap_raw[];
-    unsigned char *smem = reinterpret_cast<unsigned char *>(((uintptr_t)ap_raw + 1023) & ~(uintptr_t)1023);
+    extern __shared__ __align__(1024) unsigned char smem[]; // swizzled tiles: 1024-byte aligned (there is no static shared memory)
     ApShared *sh = reinterpret_cast<ApShared *>(smem + L::BARS);
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     const uint32_t s_base = tg_smem_u32(smem);
     const uint32_t b_qfull = tg_smem_u32(&sh->qfull), b_full = tg_smem_u32(sh->full), b_empty = tg_smem_u32(sh->empty), b_s = tg_smem_u32(sh->sready),
                    b_p = tg_smem_u32(sh->pready), b_o = tg_smem_u32(sh->odone);
-    if (warp == 0) ap_find_tile(a, blockIdx.x, lane, sh);
+    if (warp == 0) ap_find_tile(a, blockIdx.x / a.n_head, lane, sh);
     if (tid == 32) {
         ap_init(b_qfull, 1);
-        ap_init(tg_smem_u32(&sh->drain), 1);
         for (int i = 0; i < NST; ++i) { ap_init(b_full + 8 * i, 1); ap_init(b_empty + 8 * i, 1); }
-        for (int i = 0; i < 2; ++i) { ap_init(b_s + 8 * i, 1); ap_init(b_p + 8 * i, 4); ap_init(b_o + 8 * i, 1); }
+        for (int i = 0; i < 2; ++i) { ap_init(b_s + 8 * i, 1); ap_init(b_o + 8 * i, 1); }
+        ap_init(tg_smem_u32(&sh->drain), 1);
+        for (int i = 0; i < 4; ++i) ap_init(b_p + 8 * i, 8); // sub-tile 0 first and second step, sub-tile 1
         sh->abort = 0;
         sh->poison = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
-    if (sh->seq < 0) return; // no such tile
+    if (sh->tile < 0) return; // no such tile
     const int row0 = sh->tile * 2 * AP_ROWS, nq = sh->nq, nk = sh->nk, q0 = sh->q0, k0 = sh->k0, off = nk - nq;
-    const int head = blockIdx.y, kvh = head / a.group;
+    const int head = blockIdx.x % a.n_head, kvh = head / a.group;
     // key tiles of each sub-tile: up to what its last row sees
     int nt[2];
 #pragma unroll
@@ -220,7 +306,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     }
     const int n_tiles = max(nt[0], nt[1]);
     const int masked_from = min(max(off + row0 + 1, 0), nk) / AP_ROWS; // first tile with a key that some row of the block does not see
-    if (warp == 9) {
+    if (warp == 17) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tg_smem_u32(&sh->tmem)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -230,7 +316,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     const uint32_t tmem = sh->tmem; // S0 | S1 | O0 | O1, 128 columns each
     int *abort = &sh->abort;
 
-    if (warp == 8) {
+    if (warp == 16) {
         if (lane == 0 && n_tiles > 0) { // ---- TMA
             ap_expect(b_qfull, ((nt[0] > 0) + (nt[1] > 0)) * L::TILE);
 #pragma unroll
@@ -253,158 +339,205 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                 for (int n = max(0, issued - NST); n < issued; ++n) ap_wait(b_full + 8 * (n % NST), (n / NST) & 1, &mine, a.status);
             }
         }
-    } else if (warp == 9) {
-        if (lane == 0 && n_tiles > 0) { // ---- MMA
+    } else if (warp > 16) {
+        if (n_tiles > 0 && warp == 17) { // ---- MMA: the whole warp, see ap_mma_ss
             const uint32_t fmt = (1u << 4) | (BF ? (1u << 7) | (1u << 10) : 0u) | ((uint32_t)(AP_ROWS >> 4) << 24);
             const uint32_t id_s = fmt | ((uint32_t)(AP_ROWS >> 3) << 17), id_o = fmt | (1u << 16) | ((uint32_t)(HDP >> 3) << 17);
-            auto scores = [&](int s, int j) {
-                const uint32_t q = s_base + L::Q + s * L::TILE, k = s_base + L::RING + (2 * j % NST) * L::TILE;
+            const int nt0 = __shfl_sync(0xffffffffu, nt[0], 0), nt1 = __shfl_sync(0xffffffffu, nt[1], 0), n_all = max(nt0, nt1);
+            const uint32_t base = __shfl_sync(0xffffffffu, s_base, 0), td = __shfl_sync(0xffffffffu, tmem, 0);
+            auto scores = [&](int s, int stage) { // of the keys in ring stage `stage`
+                const uint32_t q = base + L::Q + s * L::TILE, k = base + L::RING + stage * L::TILE;
 #pragma unroll
                 for (int e = 0; e < HDP / 16; ++e) {
                     const uint32_t o = (e / 4) * (AP_ROWS * 128) + (e % 4) * 32;
-                    tg_mma(tmem + s * 128, tg_desc(q + o), tg_desc(k + o), id_s, e > 0);
+                    ap_mma_ss(td + s * 128, ap_desc(q + o), ap_desc(k + o), id_s, e > 0);
                 }
-                tg_commit(b_s + 8 * s);
+                ap_commit(b_s + 8 * s);
             };
-            bool ok = ap_wait(b_qfull, 0, abort, a.status) && ap_wait(b_full, 0, abort, a.status);
+            bool ok = ap_wait_warp(b_qfull, 0, abort, a.status) && ap_wait_warp(b_full, 0, abort, a.status);
             if (ok) {
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                for (int s = 0; s < 2; ++s)
-                    if (nt[s] > 0) scores(s, 0);
-                tg_commit(b_empty);
+                if (nt0 > 0) scores(0, 0);
+                if (nt1 > 0) scores(1, 0);
+                ap_commit(b_empty);
             }
-            for (int j = 0; j < n_tiles && ok; ++j) {
-                const int nv = 2 * j + 1, nk1 = 2 * j + 2;
-                ok = ap_wait(b_full + 8 * (nv % NST), (nv / NST) & 1, abort, a.status);
-                for (int s = 0; s < 2 && ok; ++s) {
-                    if (j >= nt[s]) continue;
-                    ok = ap_wait(b_p + 8 * s, j & 1, abort, a.status);
-                    if (!ok) break;
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t v = s_base + L::RING + (nv % NST) * L::TILE;
+            int sv = 1, pv = 0; // ring stage of the tile's values and its parity
+            for (int j = 0; j < n_all && ok; ++j) {
+                const int sk = sv + 1 == NST ? 0 : sv + 1, pk = sv + 1 == NST ? pv ^ 1 : pv; // the next tile's keys
+                ok = ap_wait_warp(b_full + 8 * sv, pv, abort, a.status);
+                const uint32_t v = base + L::RING + sv * L::TILE;
+                const bool more = j + 1 < n_all;
 #pragma unroll
-                    for (int e = 0; e < AP_ROWS / 16; ++e)
-                        ap_mma_ts(tmem + 256 + s * 128, tmem + s * 128 + e * 8, ap_desc_mn(v + e * 2048), id_o, j > 0 || e > 0);
-                    if (j + 1 < nt[s]) {
-                        ok = ap_wait(b_full + 8 * (nk1 % NST), (nk1 / NST) & 1, abort, a.status);
+                for (int s = 0; s < 2; ++s) {
+                    if (j >= (s ? nt1 : nt0) || !ok) continue;
+                    // weights of the keys 0-31 and 64-95, then of the others
+#pragma unroll
+                    for (int step = 0; step < 2; ++step) {
+                        ok = ok && ap_wait_warp(b_p + 16 * s + 8 * step, j & 1, abort, a.status);
                         if (!ok) break;
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                        scores(s, j + 1);
-                    } else tg_commit(b_o + 8 * s);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int e = 2 * step + (i & 1) + (i >> 1) * 4; // 16 keys
+                            ap_mma_ts(td + 256 + s * 128, td + s * 128 + e * 8, ap_desc_mn(v + e * 2048), id_o, j > 0 || step > 0 || i > 0);
+                        }
+                    }
+                    if (!ok) continue;
+                    if (j + 1 < (s ? nt1 : nt0)) {
+                        ok = ap_wait_warp(b_full + 8 * sk, pk, abort, a.status);
+                        if (!ok) continue;
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        scores(s, sk);
+                    } else ap_commit(b_o + 8 * s);
                 }
                 if (!ok) break;
-                tg_commit(b_empty + 8 * (nv % NST));
-                if (j + 1 < n_tiles) tg_commit(b_empty + 8 * (nk1 % NST));
+                ap_commit(b_empty + 8 * sv);
+                if (more) ap_commit(b_empty + 8 * sk);
+                sv = sk + 1 == NST ? 0 : sk + 1;
+                pv = sk + 1 == NST ? pk ^ 1 : pk;
             }
             if (!ok) { // no product may still run when the block goes
                 int mine = 0;
-                tg_commit(tg_smem_u32(&sh->drain));
-                ap_wait(tg_smem_u32(&sh->drain), 0, &mine, a.status);
+                ap_commit(tg_smem_u32(&sh->drain));
+                ap_wait_warp(tg_smem_u32(&sh->drain), 0, &mine, a.status);
             }
         }
     } else {
-        // ---- softmax: warps 0-3 sub-tile 0, warps 4-7 sub-tile 1; thread = row = tensor memory lane
-        const int s = warp >> 2, r = (warp & 3) * 32 + lane, row = row0 + s * AP_ROWS + r; // row of the sequence
+        // ---- softmax: sub-tile s, half of the keys of a tile; thread = row = tensor memory lane
+        const int s = warp >> 3, half = (warp >> 2) & 1, r = (warp & 3) * 32 + lane, row = row0 + s * AP_ROWS + r; // row of the sequence
         const uint32_t lanes = (uint32_t)(warp & 3) << 21, t_s = tmem + lanes + s * 128, t_o = tmem + lanes + 256 + s * 128;
+        const int two = 1 + s * 4 + (warp & 3);  // named barrier of the two warps that share 32 rows
         const int seen = min(off + row + 1, nk); // keys this row sees (also for rows behind the sequence: never stored)
         const int n_mine = s ? nt[1] : nt[0];
         const float c = a.scale_log2e;
-        float m = -INFINITY, l = 0.f; // maximum of the raw scores that the weights refer to, sum of the weights
+        float m = -INFINITY, l = 0.f; // what the weights refer to (in raw scores), sum of this thread's weights
         bool ok = true;
         for (int j = 0; j < n_mine; ++j) {
             ok = ap_wait(b_s + 8 * s, j & 1, abort, a.status);
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            uint32_t x[128];
-            ap_ld32(x, 0, t_s);
-            ap_ld32(x, 32, t_s + 32);
-            ap_ld32(x, 64, t_s + 64);
-            ap_ld32(x, 96, t_s + 96);
+            uint32_t x[64];
+            ap_ld32(x, 0, t_s + 64 * half);
+            ap_ld32(x, 32, t_s + 64 * half + 32);
             ap_wait_ld();
-            const int here = seen - j * AP_ROWS;
-            if (__any_sync(0xffffffffu, here < AP_ROWS)) {
+            const int here = seen - j * AP_ROWS - 64 * half; // this half's keys that the row sees
+            const bool masked = __any_sync(0xffffffffu, here < 64);
+            if (masked) {
 #pragma unroll
-                for (int e = 0; e < 128; ++e)
+                for (int e = 0; e < 64; ++e)
                     if (e >= here) x[e] = 0xff800000u;
             }
-            float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            float t4[4];
 #pragma unroll
-            for (int e = 0; e < 128; e += 8)
+            for (int u = 0; u < 4; ++u) t4[u] = ap_max_nan(__uint_as_float(x[u]), __uint_as_float(x[4 + u]), __uint_as_float(x[8 + u]));
 #pragma unroll
-                for (int u = 0; u < 4; ++u) t4[u] = fmaxf(t4[u], fmaxf(__uint_as_float(x[e + u]), __uint_as_float(x[e + 4 + u])));
-            const float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
+            for (int e = 12; e < 60; e += 8)
+#pragma unroll
+                for (int u = 0; u < 4; ++u) t4[u] = ap_max_nan(t4[u], __uint_as_float(x[e + u]), __uint_as_float(x[e + 4 + u]));
+#pragma unroll
+            for (int u = 0; u < 4; ++u) t4[u] = ap_max_nan(t4[u], __uint_as_float(x[60 + u]), t4[u]);
+            float top = ap_max_nan(ap_max_nan(t4[0], t4[1], t4[2]), t4[3], t4[3]);
+            if (!(top < INFINITY)) l = __uint_as_float(0x7fc00000u); // a score of +inf or NaN: the row is NaN
+            // Does any row of the two warps need another reference?  (The barrier also says that both have read their scores,
+            // whose tensor memory the weights are about to overwrite.)
             const bool rise = m == -INFINITY ? top > -INFINITY : (top - m) * c > 8.f;
-            if (__any_sync(0xffffffffu, rise)) {
-                const float f = rise ? (m == -INFINITY ? 0.f : ap_exp2((m - top) * c)) : 1.f;
-                if (rise) m = top;
+            int any;
+            asm volatile("{\n .reg .pred p, q;\n setp.ne.b32 q, %1, 0;\n barrier.cta.red.or.pred p, %2, 64, q;\n selp.b32 %0, 1, 0, p;\n}\n"
+                         : "=r"(any) : "r"((int)rise), "r"(two) : "memory");
+            if (any) {
+                sh->row[s][half][r] = top;
+                asm volatile("barrier.cta.sync %0, 64;" ::"r"(two) : "memory");
+                const float other = sh->row[s][half ^ 1][r], high = fmaxf(top, other); // (a NaN is dropped: its row's sum is NaN already)
+                const bool up = m == -INFINITY ? high > -INFINITY : (high - m) * c > 8.f;
+                const float f = up ? (m == -INFINITY ? 0.f : ap_exp2((m - high) * c)) : 1.f;
+                if (up) m = high;
                 l *= f;
-                if (j > 0) {
+                if (j > 0) { // half of O's columns each; the product that reads the weights of this tile comes after both have arrived
 #pragma unroll 1
-                    for (int o = 0; o < HDP; o += 32) {
-                        uint32_t y[32];
-                        ap_ld32(y, 0, t_o + o);
+                    for (int o = half * (HDP / 2); o < (half + 1) * (HDP / 2); o += 16) { // (16 at a time: the 64 scores are held meanwhile)
+                        uint32_t y[16];
+                        ap_ld16(y, t_o + o);
                         ap_wait_ld();
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) y[e] = __float_as_uint(__uint_as_float(y[e]) * f);
-                        ap_st32(t_o + o, y, 0);
+                        for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(__uint_as_float(y[e]) * f);
+                        ap_st16(t_o + o, y, 0);
                     }
+                    ap_wait_st();
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 }
+                asm volatile("barrier.cta.sync %0, 64;" ::"r"(two) : "memory"); // O is rescaled, and row[] may be written again
             }
-            const float ref = m == -INFINITY ? 0.f : m * c;
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int e = 0; e < 128; e += 2) {
-                const float p0 = ap_exp2(fmaf(__uint_as_float(x[e]), c, -ref)), p1 = ap_exp2(fmaf(__uint_as_float(x[e + 1]), c, -ref));
-                sum[e % 4] += p0;
-                sum[e % 4 + 1] += p1;
-                x[e / 2] = ap_pack<T>(p0, p1);
-            }
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-            ap_st32(t_s, x, 0);
-            ap_st32(t_s + 32, x, 32);
-            if (j >= masked_from) { // values of this tile that may meet a weight of zero: infinities and NaN out
+            if (j >= masked_from) { // values of this tile that may meet a weight of zero: infinities and NaN out (the 64 rows of this half)
                 const int nv = 2 * j + 1;
                 ok = ap_wait(b_full + 8 * (nv % NST), (nv / NST) & 1, abort, a.status);
                 if (!ok) break;
-                unsigned char *v = smem + L::RING + (nv % NST) * L::TILE + r * 128;
+                unsigned char *v = smem + L::RING + (nv % NST) * L::TILE + (64 * half + (r >> 1)) * 128; // two threads a row
+                constexpr int PART = HDP / 16; // 16-byte chunks each
+                const int c0 = (r & 1) * PART;
+                uint32_t bad = 0;
 #pragma unroll
-                for (int b = 0; b < HDP / 64; ++b) {
-                    uint32_t bad = 0;
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        const uint4 w = *(const uint4 *)(v + b * (AP_ROWS * 128) + ((q ^ lane) & 7) * 16);
-                        bad |= ap_nonfinite<T>(w.x) | ap_nonfinite<T>(w.y) | ap_nonfinite<T>(w.z) | ap_nonfinite<T>(w.w);
+                for (int q = 0; q < PART; ++q) {
+                    const int ch = c0 + ((q + lane) & (PART - 1));
+                    const uint4 w = *(const uint4 *)(v + (ch >> 3) * (AP_ROWS * 128) + (ch & 7) * 16);
+                    bad |= ap_nonfinite<T>(w.x) | ap_nonfinite<T>(w.y) | ap_nonfinite<T>(w.z) | ap_nonfinite<T>(w.w);
+                }
+                if (bad) {
+                    *(volatile int *)&sh->poison = 1;
+                    __threadfence_block();
+                    for (int q = c0 * 4; q < (c0 + PART) * 4; ++q) {
+                        uint32_t *w = (uint32_t *)(v + (q >> 5) * (AP_ROWS * 128)) + (q & 31);
+                        const uint32_t f = ap_nonfinite<T>(*w);
+                        if (f) *w &= ~((f >> 15) * 0xffffu);
                     }
-                    if (bad) {
-                        *(volatile int *)&sh->poison = 1;
-                        __threadfence_block();
-                        for (int q = 0; q < 32; ++q) {
-                            uint32_t *w = (uint32_t *)(v + b * (AP_ROWS * 128)) + q;
-                            const uint32_t f = ap_nonfinite<T>(*w);
-                            if (f) *w &= ~((f >> 15) * 0xffffu);
-                        }
-                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
             }
-            ap_wait_st();
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) ap_arrive(b_p + 8 * s);
+            const float ref = m == -INFINITY ? 0.f : m * c;
+            const ap_f2 c2 = ap_pair(c, c), r2 = ap_pair(-ref, -ref);
+            ap_f2 sum0 = ap_pair(0.f, 0.f), sum1 = sum0;
+            // AP_POLY of 8 exponentials on the exponential unit, the others on the multiply-add pipe (not where masked scores have to
+            // give exact zeros, or the row has no finite score yet)
+            auto weights = [&](auto poly) {
+#pragma unroll
+                for (int step = 0; step < 2; ++step) {
+#pragma unroll
+                    for (int e = 32 * step; e < 32 * step + 32; e += 2) {
+                        const ap_f2 y = ap_fma2(ap_pair(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), c2, r2);
+                        float p0, p1;
+                        if (decltype(poly)::value && e % 8 >= AP_POLY) ap_exp2_poly<T>(y, p0, p1);
+                        else { ap_unpair(y, p0, p1); p0 = ap_exp2(p0); p1 = ap_exp2(p1); }
+                        if (e % 4) sum1 = ap_add2(sum1, ap_pair(p0, p1)); else sum0 = ap_add2(sum0, ap_pair(p0, p1));
+                        x[e / 2] = ap_pack<T>(p0, p1);
+                    }
+                    ap_st16(t_s + 32 * half + 16 * step, x, 16 * step);
+                    ap_wait_st();
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) ap_arrive(b_p + 16 * s + 8 * step);
+                }
+            };
+            if (AP_POLY < 8 && !masked && !__any_sync(0xffffffffu, m == -INFINITY)) weights(std::true_type());
+            else weights(std::false_type());
+            {
+                float s0, s1;
+                ap_unpair(ap_add2(sum0, sum1), s0, s1);
+                l += s0 + s1;
+            }
         }
-        // ---- output
+        // ---- output: half of the columns each
         const bool valid = row < nq;
         T *out = (T *)a.out.data + (long long)(q0 + row) * a.out.row_stride + (long long)head * a.out.head_stride;
         if (n_mine == 0) {
-            if (valid)
+            if (valid && half == 0)
                 for (int e = 0; e < a.hd; e += 8) *(uint4 *)(out + e) = make_uint4(0, 0, 0, 0);
         } else if (ok && ap_wait(b_o + 8 * s, 0, abort, a.status)) {
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            asm volatile("bar.sync %0, 128;" ::"r"(1 + s) : "memory"); // all of this sub-tile's looks at the values are done
+            sh->row[s][half][r] = l;
+            asm volatile("barrier.cta.sync %0, 256;" ::"r"(9 + s) : "memory"); // the sums; and all of this sub-tile's looks at the values are done
             const bool poison = *(volatile int *)&sh->poison;
-            const float inv = seen > 0 ? 1.f / l : 0.f;
+            const float inv = seen > 0 ? 1.f / (sh->row[s][0][r] + sh->row[s][1][r]) : 0.f;
 #pragma unroll 1
-            for (int o = 0; o < HDP; o += 32) {
+            for (int o = half * (HDP / 2); o < (half + 1) * (HDP / 2); o += 32) {
                 uint32_t y[32];
                 ap_ld32(y, 0, t_o + o);
                 ap_wait_ld();
@@ -441,7 +574,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
-    if (warp == 9) {
+    if (warp == 17) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
     }
@@ -511,9 +644,11 @@ extern "C" int mdi_attn_prompt(int n_seq, const int32_t *q_start_dev, const int3
     if (e != CUDA_SUCCESS) return op_fail(MDI_ERR_SHAPE, "%s: no tensor map for these rows and strides (%d)", who, (int)e);
     a.v = op_rows(v); a.out = op_rows(out);
     a.q_start = q_start_dev; a.k_start = k_start_dev; a.status = status_dev;
-    a.n_seq = n_seq; a.n_q = n_q_rows; a.n_k = n_k_rows; a.group = n_head / n_kv_head; a.hd = head_dim;
+    a.n_seq = n_seq; a.n_q = n_q_rows; a.n_k = n_k_rows; a.n_head = n_head; a.group = n_head / n_kv_head; a.hd = head_dim;
     a.scale_log2e = scale * 1.4426950408889634f;
-    const dim3 grid((unsigned)(n_q_rows / (2 * AP_ROWS) + std::min(n_seq, n_q_rows)), n_head);
+    const int64_t blocks = ((int64_t)n_q_rows / (2 * AP_ROWS) + std::min(n_seq, n_q_rows)) * n_head;
+    if (blocks > 0x7fffffff) return op_fail(MDI_ERR_SHAPE, "%s: too many rows and heads for one call", who);
+    const dim3 grid((unsigned)blocks);
     cudaStream_t st = (cudaStream_t)stream;
     cudaError_t ce;
     if (q->dtype == MDI_DTYPE_F16) ce = head_dim == 128 ? ap_launch<__half, 128>(mq, mk, mv, a, grid, st) : ap_launch<__half, 64>(mq, mk, mv, a, grid, st);
