@@ -6,18 +6,17 @@
 //
 // One block takes 256 query rows of one head (two sub-tiles of 128) and walks the keys its rows see in tiles of 128, once:
 //   warp 16     requests the tiles by TMA (128-byte swizzle, no multicast): queries once, then keys and values through one ring;
-//   warp 17     issues tcgen05.mma: scores S = Q K^T (128 x 128) and outputs O += P V, accumulators in tensor memory, in the fixed
-//               order P0 V, next S0, P1 V, next S1: one sub-tile's products run while the other's softmax does.  (With a warp for each
-//               sub-tile the products interleave, both softmaxes start together and wait for the exponential unit together: a tile
-//               took 5500 clocks instead of the [[CLK]].)
-//   warps 0-7, 8-15  softmax of sub-tile 0 and 1.  A row belongs to two threads, 64 keys of a tile each (one thread per row left the
-//               schedulers with two warps each and waited for latencies: 1.7x the time): scores from tensor memory, maximum and sum
-//               in fp32, weights rounded to the type of V back into the tensor memory of the scores (an A operand is read from
-//               there) in two steps, so that the product of the first half runs while the second is computed.  Weights refer to a
-//               maximum that both threads of a row hold; it moves, and what has been summed in O is rescaled, only when a score exceeds it by 2^8
-//               (weights stay below that; sums are fp32), so the two hardly ever talk and O hardly ever leaves tensor memory.
-// The scores' accumulator ready implies that the sub-tile's previous output product is complete (both are committed in order),
-// which is what makes the rescaling safe.
+//   warps 17, 18 issue tcgen05.mma, accumulators in tensor memory: one the scores S = Q K^T (128 x 128), the other the outputs O += P V.
+//               Both sub-tiles share one S: it is in use only until the softmax has taken the scores into registers, and the next
+//               ones are asked for at once, so they are there when a softmax has done its tile; none waits for a product of weights
+//               and values.  It also keeps the sub-tiles out of step, so that one's products run while the other's exponentials do (an
+//               S each, where head_dim 64 leaves room for it: 462 instead of 419 us for 8192 tokens and 32 heads).
+//   warps 0-7, 8-15  softmax of sub-tile 0 and 1.  A row belongs to two threads, 64 keys of a tile each (with one thread per row the
+//               schedulers have two warps each and wait for latencies): maximum and sum in fp32, weights rounded to the type of V
+//               into tensor memory (an A operand is read from there) in two steps, so that the product of the first half runs while
+//               the second is computed.  Weights refer to a maximum that both threads of a row hold; it moves, and what has been
+//               summed in O is rescaled, only when a score exceeds it by 2^8 (weights stay below that; sums are fp32), so the two
+//               threads hardly ever exchange more than a vote and O hardly ever leaves tensor memory.
 //
 // Masked places: scores of keys a row does not see are replaced, so whatever they hold has no effect.  Values meet a weight of
 // zero, which an infinity or a NaN would survive: in the tiles where anything is masked, such values are replaced by zero in
@@ -34,9 +33,6 @@
 namespace mdi {
 namespace {
 
-#ifndef AP_POLY
-#define AP_POLY 6
-#endif
 constexpr int AP_ROWS = 128;              // rows of a sub-tile, keys of a tile
 constexpr int AP_THREADS = 640;
 constexpr int AP_SORT = 64;               // up to this many sequences their tiles are taken in order of the keys they see
@@ -54,12 +50,14 @@ struct ApArgs {
 template <int HDP> struct ApLayout {
     static constexpr int TILE = AP_ROWS * HDP * 2;
     static constexpr int STAGES = HDP == 128 ? 5 : 8;
+    // columns of tensor memory: scores, weights of sub-tile s at P + 64 s, outputs at O + HDP s
+    static constexpr int P = 128, O = 256;
     static constexpr int Q = 0, RING = 2 * TILE, BARS = RING + STAGES * TILE;
     static constexpr int SMEM = BARS + 2560; // barriers and what threads tell each other
 };
 
 struct ApShared { // behind the ring
-    unsigned long long qfull, full[8], empty[8], sready[2], pready[4], odone[2], drain;
+    unsigned long long qfull, full[8], empty[8], sready[2], sfree, pready[4], pvdone[2], drain[2];
     unsigned tmem;
     int abort, poison;
     float row[2][2][AP_ROWS];      // [sub-tile][half][row]: what the two threads of a row tell each other
@@ -72,23 +70,28 @@ __device__ __forceinline__ void ap_arrive(uint32_t bar) { asm volatile("mbarrier
 __device__ __forceinline__ void ap_expect(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-// false: the wait gave up, or another one of the block did
-__device__ __noinline__ bool ap_wait_slow(uint32_t bar, uint32_t parity, int *abort, int *status) {
+// false: the wait gave up, or another one of the block did.  SLEEP: the thread may sleep between its looks; waking up then takes some
+// 180 clocks longer, but a sleeping warp takes no issue slots from the softmax warps of the other sub-tile.
+template <bool SLEEP> __device__ __noinline__ bool ap_wait_slow(uint32_t bar, uint32_t parity, int *abort, int *status) {
     const unsigned long long t0 = tg_now();
-    for (;;) {
-        uint32_t done; // the thread may sleep for up to 20 us: polling takes issue slots from the softmax
-        asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n selp.u32 %0, 1, 0, p;\n}\n"
-                     : "=r"(done) : "r"(bar), "r"(parity), "r"(20000) : "memory");
-        if (done) return true;
-        if (*(volatile int *)abort) return false;
-        if (tg_now() - t0 > AP_WAIT_NS) break;
+    for (unsigned it = 0;; ++it) {
+        if (SLEEP) {
+            uint32_t done;
+            asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n selp.u32 %0, 1, 0, p;\n}\n"
+                         : "=r"(done) : "r"(bar), "r"(parity), "r"(20000) : "memory"); // ns
+            if (done) return true;
+        } else if (tg_try_wait(bar, parity)) return true;
+        if (SLEEP || (it & 15u) == 15u) {
+            if (*(volatile int *)abort) return false;
+            if (tg_now() - t0 > AP_WAIT_NS) break;
+        }
     }
     *(volatile int *)abort = 1;
     op_status(status, MDI_STATUS_TIMEOUT);
     return false;
 }
 __device__ __forceinline__ bool ap_wait(uint32_t bar, uint32_t parity, int *abort, int *status) {
-    return tg_try_wait(bar, parity) || ap_wait_slow(bar, parity, abort, status);
+    return tg_try_wait(bar, parity) || ap_wait_slow<true>(bar, parity, abort, status);
 }
 __device__ __forceinline__ void ap_tma(uint32_t dst, const CUtensorMap *map, int c0, int c1, int c2, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
@@ -101,10 +104,18 @@ template <int HDP> __device__ __forceinline__ void ap_load(uint32_t dst, const C
 }
 // ---- issued by a whole warp in step (one elected lane): the compiler can then keep descriptors in uniform registers; with one
 // thread of a diverged warp issuing, moving them there took longer than the products (90 instead of 64 clocks each)
-__device__ __forceinline__ bool ap_wait_warp(uint32_t bar, uint32_t parity, int *abort, int *status) {
+template <bool SLEEP = true> __device__ __forceinline__ bool ap_wait_warp(uint32_t bar, uint32_t parity, int *abort, int *status) {
     bool ok = tg_try_wait(bar, parity);
-    if (!__all_sync(0xffffffffu, ok)) ok = ok || ap_wait_slow(bar, parity, abort, status);
+    if (!__all_sync(0xffffffffu, ok)) ok = ok || ap_wait_slow<SLEEP>(bar, parity, abort, status);
     return __all_sync(0xffffffffu, ok);
+}
+// named barriers of the softmax warps
+__device__ __forceinline__ void ap_meet(int bar, int threads) { asm volatile("barrier.cta.sync %0, %1;" ::"r"(bar), "r"(threads) : "memory"); }
+__device__ __forceinline__ bool ap_vote(int bar, bool yes) { // of 64 threads
+    int any;
+    asm volatile("{\n .reg .pred p, q;\n setp.ne.b32 q, %1, 0;\n barrier.cta.red.or.pred p, %2, 64, q;\n selp.b32 %0, 1, 0, p;\n}\n"
+                 : "=r"(any) : "r"((int)yes), "r"(bar) : "memory");
+    return any != 0;
 }
 // Shared-memory descriptors.  Queries and keys: rows of 128 bytes along head_dim, 128-byte swizzle, 8 rows = 1024 bytes.  Values: the
 // rows run along the reduction (keys), the next 64 elements of head_dim are one box further.
@@ -166,32 +177,6 @@ __device__ __forceinline__ void ap_unpair(ap_f2 p, float &a, float &b) { asm("mo
 __device__ __forceinline__ ap_f2 ap_fma2(ap_f2 a, ap_f2 b, ap_f2 c) { ap_f2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
 __device__ __forceinline__ ap_f2 ap_add2(ap_f2 a, ap_f2 b) { ap_f2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 __device__ __forceinline__ float ap_max_nan(float a, float b, float c) { float r; asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; } // NaN if one is
-
-// 2^x on the multiply-add pipe, for x in [-125, 2^22) (below -125: 2^-125): x = n + f with f in [-1/2, 1/2], a polynomial in f
-// that is minimax in the relative error (degree 3: 7.5e-5, a 26th of bf16's half step; degree 4: 2.7e-6, for fp16; fitted by the
-// exchange algorithm), n added to its exponent.
-template <typename T> __device__ __forceinline__ void ap_exp2_poly(ap_f2 x, float &p0, float &p1) {
-    float x0, x1, t0, t1;
-    ap_unpair(x, x0, x1);
-    x = ap_pair(fmaxf(x0, -125.f), fmaxf(x1, -125.f));
-    const ap_f2 magic = ap_pair(12582912.f, 12582912.f), unmagic = ap_pair(-12582912.f, -12582912.f), minus = ap_pair(-1.f, -1.f);
-    const ap_f2 t = ap_add2(x, magic), f = ap_fma2(ap_add2(t, unmagic), minus, x);
-    ap_f2 y;
-    if constexpr (std::is_same<T, __half>::value) {
-        y = ap_fma2(f, ap_pair(0.0095701022f, 0.0095701022f), ap_pair(0.0559178591f, 0.0559178591f));
-        y = ap_fma2(y, f, ap_pair(0.2402474433f, 0.2402474433f));
-        y = ap_fma2(y, f, ap_pair(0.6931217909f, 0.6931217909f));
-        y = ap_fma2(y, f, ap_pair(0.9999992847f, 0.9999992847f));
-    } else {
-        y = ap_fma2(f, ap_pair(0.0551716685f, 0.0551716685f), ap_pair(0.2426111251f, 0.2426111251f));
-        y = ap_fma2(y, f, ap_pair(0.6932609677f, 0.6932609677f));
-        y = ap_fma2(y, f, ap_pair(0.9999280572f, 0.9999280572f));
-    }
-    ap_unpair(t, t0, t1);
-    ap_unpair(y, p0, p1);
-    p0 = __uint_as_float(__float_as_uint(p0) + (__float_as_uint(t0) << 23));
-    p1 = __uint_as_float(__float_as_uint(p1) + (__float_as_uint(t1) << 23));
-}
 
 template <typename T> __device__ __forceinline__ uint32_t ap_pack(float x, float y);
 template <> __device__ __forceinline__ uint32_t ap_pack<__half>(float x, float y) { const __half2 h = __floats2half2_rn(x, y); return *(const uint32_t *)&h; }
@@ -281,13 +266,14 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     const uint32_t s_base = tg_smem_u32(smem);
     const uint32_t b_qfull = tg_smem_u32(&sh->qfull), b_full = tg_smem_u32(sh->full), b_empty = tg_smem_u32(sh->empty), b_s = tg_smem_u32(sh->sready),
-                   b_p = tg_smem_u32(sh->pready), b_o = tg_smem_u32(sh->odone);
+                   b_p = tg_smem_u32(sh->pready), b_pv = tg_smem_u32(sh->pvdone), b_free = tg_smem_u32(&sh->sfree);
     if (warp == 0) ap_find_tile(a, blockIdx.x / a.n_head, lane, sh);
     if (tid == 32) {
         ap_init(b_qfull, 1);
         for (int i = 0; i < NST; ++i) { ap_init(b_full + 8 * i, 1); ap_init(b_empty + 8 * i, 1); }
-        for (int i = 0; i < 2; ++i) { ap_init(b_s + 8 * i, 1); ap_init(b_o + 8 * i, 1); }
-        ap_init(tg_smem_u32(&sh->drain), 1);
+        for (int i = 0; i < 2; ++i) { ap_init(b_s + 8 * i, 1); ap_init(b_pv + 8 * i, 1); }
+        ap_init(b_free, 8);
+        for (int i = 0; i < 2; ++i) ap_init(tg_smem_u32(&sh->drain[i]), 1);
         for (int i = 0; i < 4; ++i) ap_init(b_p + 8 * i, 8); // sub-tile 0 first and second step, sub-tile 1
         sh->abort = 0;
         sh->poison = 0;
@@ -313,7 +299,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    const uint32_t tmem = sh->tmem; // S0 | S1 | O0 | O1, 128 columns each
+    const uint32_t tmem = sh->tmem;
     int *abort = &sh->abort;
 
     if (warp == 16) {
@@ -340,72 +326,77 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             }
         }
     } else if (warp > 16) {
-        if (n_tiles > 0 && warp == 17) { // ---- MMA: the whole warp, see ap_mma_ss
+        if (n_tiles > 0 && warp < 19) { // ---- MMA: the whole warp, see ap_mma_ss
             const uint32_t fmt = (1u << 4) | (BF ? (1u << 7) | (1u << 10) : 0u) | ((uint32_t)(AP_ROWS >> 4) << 24);
-            const uint32_t id_s = fmt | ((uint32_t)(AP_ROWS >> 3) << 17), id_o = fmt | (1u << 16) | ((uint32_t)(HDP >> 3) << 17);
             const int nt0 = __shfl_sync(0xffffffffu, nt[0], 0), nt1 = __shfl_sync(0xffffffffu, nt[1], 0), n_all = max(nt0, nt1);
             const uint32_t base = __shfl_sync(0xffffffffu, s_base, 0), td = __shfl_sync(0xffffffffu, tmem, 0);
-            auto scores = [&](int s, int stage) { // of the keys in ring stage `stage`
-                const uint32_t q = base + L::Q + s * L::TILE, k = base + L::RING + stage * L::TILE;
+            bool ok = true;
+            if (warp == 17) { // scores
+                const uint32_t id_s = fmt | ((uint32_t)(AP_ROWS >> 3) << 17);
+                int st = 0, par = 0, uses = 0; // ring stage of the tile's keys and its parity; uses of S so far
+                ok = ap_wait_warp(b_qfull, 0, abort, a.status);
+                for (int j = 0; j < n_all && ok; ++j) {
+                    ok = ap_wait_warp(b_full + 8 * st, par, abort, a.status);
+                    const uint32_t k = base + L::RING + st * L::TILE;
 #pragma unroll
-                for (int e = 0; e < HDP / 16; ++e) {
-                    const uint32_t o = (e / 4) * (AP_ROWS * 128) + (e % 4) * 32;
-                    ap_mma_ss(td + s * 128, ap_desc(q + o), ap_desc(k + o), id_s, e > 0);
-                }
-                ap_commit(b_s + 8 * s);
-            };
-            bool ok = ap_wait_warp(b_qfull, 0, abort, a.status) && ap_wait_warp(b_full, 0, abort, a.status);
-            if (ok) {
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                if (nt0 > 0) scores(0, 0);
-                if (nt1 > 0) scores(1, 0);
-                ap_commit(b_empty);
-            }
-            int sv = 1, pv = 0; // ring stage of the tile's values and its parity
-            for (int j = 0; j < n_all && ok; ++j) {
-                const int sk = sv + 1 == NST ? 0 : sv + 1, pk = sv + 1 == NST ? pv ^ 1 : pv; // the next tile's keys
-                ok = ap_wait_warp(b_full + 8 * sv, pv, abort, a.status);
-                const uint32_t v = base + L::RING + sv * L::TILE;
-                const bool more = j + 1 < n_all;
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    if (j >= (s ? nt1 : nt0) || !ok) continue;
-                    // weights of the keys 0-31 and 64-95, then of the others
-#pragma unroll
-                    for (int step = 0; step < 2; ++step) {
-                        ok = ok && ap_wait_warp(b_p + 16 * s + 8 * step, j & 1, abort, a.status);
-                        if (!ok) break;
-                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int e = 2 * step + (i & 1) + (i >> 1) * 4; // 16 keys
-                            ap_mma_ts(td + 256 + s * 128, td + s * 128 + e * 8, ap_desc_mn(v + e * 2048), id_o, j > 0 || step > 0 || i > 0);
-                        }
-                    }
-                    if (!ok) continue;
-                    if (j + 1 < (s ? nt1 : nt0)) {
-                        ok = ap_wait_warp(b_full + 8 * sk, pk, abort, a.status);
+                    for (int s = 0; s < 2; ++s) {
+                        if (j >= (s ? nt1 : nt0) || !ok) continue;
+                        if (uses > 0) ok = ap_wait_warp<false>(b_free, (uses - 1) & 1, abort, a.status); // the previous scores have been taken
                         if (!ok) continue;
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                        scores(s, sk);
-                    } else ap_commit(b_o + 8 * s);
+                        const uint32_t q = base + L::Q + s * L::TILE;
+#pragma unroll
+                        for (int e = 0; e < HDP / 16; ++e) {
+                            const uint32_t o = (e / 4) * (AP_ROWS * 128) + (e % 4) * 32;
+                            ap_mma_ss(td, ap_desc(q + o), ap_desc(k + o), id_s, e > 0);
+                        }
+                        ap_commit(b_s + 8 * s);
+                        ++uses;
+                    }
+                    if (!ok) break;
+                    ap_commit(b_empty + 8 * st);
+                    st += 2;
+                    if (st >= NST) { st -= NST; par ^= 1; }
                 }
-                if (!ok) break;
-                ap_commit(b_empty + 8 * sv);
-                if (more) ap_commit(b_empty + 8 * sk);
-                sv = sk + 1 == NST ? 0 : sk + 1;
-                pv = sk + 1 == NST ? pk ^ 1 : pk;
+            } else { // outputs
+                const uint32_t id_o = fmt | (1u << 16) | ((uint32_t)(HDP >> 3) << 17);
+                int st = 1, par = 0;
+                for (int j = 0; j < n_all && ok; ++j) {
+                    ok = ap_wait_warp(b_full + 8 * st, par, abort, a.status);
+                    const uint32_t v = base + L::RING + st * L::TILE;
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        if (j >= (s ? nt1 : nt0)) continue;
+                        // weights of the keys 0-31 and 64-95, then of the others
+#pragma unroll
+                        for (int step = 0; step < 2; ++step) {
+                            ok = ok && ap_wait_warp<false>(b_p + 16 * s + 8 * step, j & 1, abort, a.status);
+                            if (!ok) break;
+                            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const int e = 2 * step + (i & 1) + (i >> 1) * 4; // 16 keys
+                                ap_mma_ts(td + L::O + s * HDP, td + L::P + s * 64 + e * 8, ap_desc_mn(v + e * 2048), id_o, j > 0 || step > 0 || i > 0);
+                            }
+                        }
+                        if (ok) ap_commit(b_pv + 8 * s);
+                    }
+                    if (!ok) break;
+                    ap_commit(b_empty + 8 * st);
+                    st += 2;
+                    if (st >= NST) { st -= NST; par ^= 1; }
+                }
             }
             if (!ok) { // no product may still run when the block goes
                 int mine = 0;
-                ap_commit(tg_smem_u32(&sh->drain));
-                ap_wait_warp(tg_smem_u32(&sh->drain), 0, &mine, a.status);
+                ap_commit(tg_smem_u32(&sh->drain[warp - 17]));
+                ap_wait_warp(tg_smem_u32(&sh->drain[warp - 17]), 0, &mine, a.status);
             }
         }
     } else {
         // ---- softmax: sub-tile s, half of the keys of a tile; thread = row = tensor memory lane
         const int s = warp >> 3, half = (warp >> 2) & 1, r = (warp & 3) * 32 + lane, row = row0 + s * AP_ROWS + r; // row of the sequence
-        const uint32_t lanes = (uint32_t)(warp & 3) << 21, t_s = tmem + lanes + s * 128, t_o = tmem + lanes + 256 + s * 128;
+        const uint32_t lanes = (uint32_t)(warp & 3) << 21, t_s = tmem + lanes + 64 * half, t_p = tmem + lanes + L::P + s * 64 + 32 * half, t_o = tmem + lanes + L::O + s * HDP;
         const int two = 1 + s * 4 + (warp & 3);  // named barrier of the two warps that share 32 rows
         const int seen = min(off + row + 1, nk); // keys this row sees (also for rows behind the sequence: never stored)
         const int n_mine = s ? nt[1] : nt[0];
@@ -413,16 +404,22 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         float m = -INFINITY, l = 0.f; // what the weights refer to (in raw scores), sum of this thread's weights
         bool ok = true;
         for (int j = 0; j < n_mine; ++j) {
-            ok = ap_wait(b_s + 8 * s, j & 1, abort, a.status);
-            if (!ok) break;
+            // (after a wait that ran out a warp goes on to meet its partner at the barriers, and does nothing else)
+            ok = ok && ap_wait_warp(b_s + 8 * s, j & 1, abort, a.status);
+            if (!ok) {
+                if (ap_vote(two, false)) { ap_meet(two, 64); ap_meet(two, 64); }
+                continue;
+            }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             uint32_t x[64];
-            ap_ld32(x, 0, t_s + 64 * half);
-            ap_ld32(x, 32, t_s + 64 * half + 32);
+            ap_ld32(x, 0, t_s);
+            ap_ld32(x, 32, t_s + 32);
             ap_wait_ld();
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) ap_arrive(b_free); // S may hold the other sub-tile's scores
             const int here = seen - j * AP_ROWS - 64 * half; // this half's keys that the row sees
-            const bool masked = __any_sync(0xffffffffu, here < 64);
-            if (masked) {
+            if (__any_sync(0xffffffffu, here < 64)) {
 #pragma unroll
                 for (int e = 0; e < 64; ++e)
                     if (e >= here) x[e] = 0xff800000u;
@@ -438,21 +435,19 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             for (int u = 0; u < 4; ++u) t4[u] = ap_max_nan(t4[u], __uint_as_float(x[60 + u]), t4[u]);
             float top = ap_max_nan(ap_max_nan(t4[0], t4[1], t4[2]), t4[3], t4[3]);
             if (!(top < INFINITY)) l = __uint_as_float(0x7fc00000u); // a score of +inf or NaN: the row is NaN
-            // Does any row of the two warps need another reference?  (The barrier also says that both have read their scores,
-            // whose tensor memory the weights are about to overwrite.)
+            // does any row of the two warps need another reference?
             const bool rise = m == -INFINITY ? top > -INFINITY : (top - m) * c > 8.f;
-            int any;
-            asm volatile("{\n .reg .pred p, q;\n setp.ne.b32 q, %1, 0;\n barrier.cta.red.or.pred p, %2, 64, q;\n selp.b32 %0, 1, 0, p;\n}\n"
-                         : "=r"(any) : "r"((int)rise), "r"(two) : "memory");
-            if (any) {
+            if (ap_vote(two, rise)) {
                 sh->row[s][half][r] = top;
-                asm volatile("barrier.cta.sync %0, 64;" ::"r"(two) : "memory");
+                ap_meet(two, 64);
                 const float other = sh->row[s][half ^ 1][r], high = fmaxf(top, other); // (a NaN is dropped: its row's sum is NaN already)
                 const bool up = m == -INFINITY ? high > -INFINITY : (high - m) * c > 8.f;
                 const float f = up ? (m == -INFINITY ? 0.f : ap_exp2((m - high) * c)) : 1.f;
                 if (up) m = high;
                 l *= f;
-                if (j > 0) { // half of O's columns each; the product that reads the weights of this tile comes after both have arrived
+                if (j > 0) { // half of O's columns each, once the product of the previous tile is in
+                    ok = ap_wait_warp(b_pv + 8 * s, (j - 1) & 1, abort, a.status);
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
                     for (int o = half * (HDP / 2); o < (half + 1) * (HDP / 2); o += 16) { // (16 at a time: the 64 scores are held meanwhile)
                         uint32_t y[16];
@@ -465,12 +460,12 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                     ap_wait_st();
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 }
-                asm volatile("barrier.cta.sync %0, 64;" ::"r"(two) : "memory"); // O is rescaled, and row[] may be written again
+                ap_meet(two, 64); // O is rescaled, and row[] may be written again
             }
             if (j >= masked_from) { // values of this tile that may meet a weight of zero: infinities and NaN out (the 64 rows of this half)
                 const int nv = 2 * j + 1;
-                ok = ap_wait(b_full + 8 * (nv % NST), (nv / NST) & 1, abort, a.status);
-                if (!ok) break;
+                ok = ok && ap_wait_warp(b_full + 8 * (nv % NST), (nv / NST) & 1, abort, a.status);
+                if (!ok) continue;
                 unsigned char *v = smem + L::RING + (nv % NST) * L::TILE + (64 * half + (r >> 1)) * 128; // two threads a row
                 constexpr int PART = HDP / 16; // 16-byte chunks each
                 const int c0 = (r & 1) * PART;
@@ -492,32 +487,34 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
             }
+            // The previous weights have been used.  (Waiting here rather than before the first store, half an exponential phase later,
+            // keeps the sub-tiles out of step: 2990 instead of 3400 clocks a tile.)
+            ok = ok && (j == 0 || ap_wait_warp(b_pv + 8 * s, (j - 1) & 1, abort, a.status));
+            if (!ok) continue;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const float ref = m == -INFINITY ? 0.f : m * c;
             const ap_f2 c2 = ap_pair(c, c), r2 = ap_pair(-ref, -ref);
             ap_f2 sum0 = ap_pair(0.f, 0.f), sum1 = sum0;
-            // AP_POLY of 8 exponentials on the exponential unit, the others on the multiply-add pipe (not where masked scores have to
-            // give exact zeros, or the row has no finite score yet)
-            auto weights = [&](auto poly) {
+            // (Replacing a quarter of the exponentials by polynomials on the multiply-add pipe made a tile 20% slower: the exponential
+            // unit is 70% busy, and the softmax warps' instructions, not it, are what the four warps of a scheduler queue for.)
 #pragma unroll
-                for (int step = 0; step < 2; ++step) {
+            for (int step = 0; step < 2; ++step) {
 #pragma unroll
-                    for (int e = 32 * step; e < 32 * step + 32; e += 2) {
-                        const ap_f2 y = ap_fma2(ap_pair(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), c2, r2);
-                        float p0, p1;
-                        if (decltype(poly)::value && e % 8 >= AP_POLY) ap_exp2_poly<T>(y, p0, p1);
-                        else { ap_unpair(y, p0, p1); p0 = ap_exp2(p0); p1 = ap_exp2(p1); }
-                        if (e % 4) sum1 = ap_add2(sum1, ap_pair(p0, p1)); else sum0 = ap_add2(sum0, ap_pair(p0, p1));
-                        x[e / 2] = ap_pack<T>(p0, p1);
-                    }
-                    ap_st16(t_s + 32 * half + 16 * step, x, 16 * step);
-                    ap_wait_st();
-                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) ap_arrive(b_p + 16 * s + 8 * step);
+                for (int e = 32 * step; e < 32 * step + 32; e += 2) {
+                    const ap_f2 y = ap_fma2(ap_pair(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), c2, r2);
+                    float p0, p1;
+                    ap_unpair(y, p0, p1);
+                    p0 = ap_exp2(p0);
+                    p1 = ap_exp2(p1);
+                    if (e % 4) sum1 = ap_add2(sum1, ap_pair(p0, p1)); else sum0 = ap_add2(sum0, ap_pair(p0, p1));
+                    x[e / 2] = ap_pack<T>(p0, p1);
                 }
-            };
-            if (AP_POLY < 8 && !masked && !__any_sync(0xffffffffu, m == -INFINITY)) weights(std::true_type());
-            else weights(std::false_type());
+                ap_st16(t_p + 16 * step, x, 16 * step);
+                ap_wait_st();
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) ap_arrive(b_p + 16 * s + 8 * step);
+            }
             {
                 float s0, s1;
                 ap_unpair(ap_add2(sum0, sum1), s0, s1);
@@ -530,14 +527,15 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         if (n_mine == 0) {
             if (valid && half == 0)
                 for (int e = 0; e < a.hd; e += 8) *(uint4 *)(out + e) = make_uint4(0, 0, 0, 0);
-        } else if (ok && ap_wait(b_o + 8 * s, 0, abort, a.status)) {
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        } else {
             sh->row[s][half][r] = l;
-            asm volatile("barrier.cta.sync %0, 256;" ::"r"(9 + s) : "memory"); // the sums; and all of this sub-tile's looks at the values are done
+            ap_meet(9 + s, 256); // the sums; and all of this sub-tile's looks at the values are done
+            ok = ok && ap_wait_warp(b_pv + 8 * s, (n_mine - 1) & 1, abort, a.status);
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const bool poison = *(volatile int *)&sh->poison;
             const float inv = seen > 0 ? 1.f / (sh->row[s][0][r] + sh->row[s][1][r]) : 0.f;
 #pragma unroll 1
-            for (int o = half * (HDP / 2); o < (half + 1) * (HDP / 2); o += 32) {
+            for (int o = half * (HDP / 2); o < (half + 1) * (HDP / 2) && ok; o += 32) {
                 uint32_t y[32];
                 ap_ld32(y, 0, t_o + o);
                 ap_wait_ld();
