@@ -365,7 +365,7 @@ def main():
     ap.add_argument("--rounds-per-graph", type=int, default=0)
     ap.add_argument("--scheduler", type=int, default=0, help="0 auto (a persistent kernel when the shape fits), 1 streams, 2 phase-per-matrix persistent kernel, 3 fused-phase persistent kernel")
     ap.add_argument("--tc-min-group", type=int, default=0, help="smallest group whose decode steps run on the tensor cores (0 = library default)")
-    ap.add_argument("--kv-cache-dtype", type=int, default=0, help="0 library default, 1 bf16, 2 fp16, 3 fp32")
+    ap.add_argument("--kv-cache-dtype", type=int, default=0, help="0 library default, 1 bf16, 2 fp16, 3 fp32, 4 int8, 5 e4m3")
     ap.add_argument("--in-kernel-timing", action="store_true", help="persistent kernels time themselves; adds partition_times_ms "
                     "(per partition: blocks, milliseconds per category of the last generate call) to the line")
     ap.add_argument("--fused-blocks-per-head", type=int, default=0, help="scheduler 3: 1 = one block per head (no clusters), 0 = library default")

@@ -78,7 +78,11 @@ typedef struct {
                           F16 halves the cache bytes at 1.6e-2 worst absolute logit error on the 32-block Llama-7B shape and
                           6e-4 on the 48-block GPT-2-XL shape (measured over whole generations; fp32: 1.2e-3 and 3e-5); keys
                           and values of these models are far inside its range.  BF16 costs eight times the F16 error, which
-                          on the 32-block model exceeds a 3e-2 absolute logit tolerance */
+                          on the 32-block model exceeds a 3e-2 absolute logit tolerance.  I8 and E4M3 (bf16 weights, prefill_mode 0,
+                          scheduler 0 or 1, pages of at least 16 rows; default 64): 8-bit elements with a scale per row and head
+                          (mdi_kv_cache); first visits and every step then run through the attention operators below, on the
+                          stream scheduler with tensor-core linear layers whatever the group.  They quarter an fp32 cache at the
+                          price of their rounding: see mdi_kv_append for it */
     int prefill_mode;  /* first visits (whole prompt): 0 (default) tensor-core GEMMs (tcgen05, bf16 x bf16 -> fp32, inputs split
                           into two bf16 planes) when the weights are bf16, else the CUDA-core step kernels in chunks of 8
                           positions; 1: always the CUDA-core kernels */

@@ -716,7 +716,8 @@ AdPlan ad_plan(const mdi_kv_cache *c, int n_seq, int n_head, int max_len) {
 
 template <typename RT, int ST, int HD> cudaError_t ad_launch(const AdArgs &a, int blocks, cudaStream_t st) {
     constexpr size_t smem = AdTile<ST, HD>::BLOCK_SMEM;
-    cudaError_t e = cudaFuncSetAttribute(k_attn_decode_op<RT, ST, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    static OpOnce once;
+    cudaError_t e = once([] { return cudaFuncSetAttribute(k_attn_decode_op<RT, ST, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
     if (e != cudaSuccess) return e;
     k_attn_decode_op<RT, ST, HD><<<blocks, AD_THREADS, smem, st>>>(a);
     if ((e = cudaGetLastError()) != cudaSuccess) return e;

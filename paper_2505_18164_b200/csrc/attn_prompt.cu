@@ -598,8 +598,8 @@ CUresult ap_make_map(CUtensorMap *map, const mdi_rows *r, int rows, int heads, i
 
 template <typename T, int HDP>
 cudaError_t ap_launch(const CUtensorMap &mq, const CUtensorMap &mk, const CUtensorMap &mv, const ApArgs &a, dim3 grid, cudaStream_t st) {
-    const cudaError_t e = cudaFuncSetAttribute(k_attn_prompt<T, HDP>, cudaFuncAttributeMaxDynamicSharedMemorySize, ApLayout<HDP>::SMEM);
-    if (e != cudaSuccess) return e;
+    static OpOnce once;
+    if (const cudaError_t e = once([] { return cudaFuncSetAttribute(k_attn_prompt<T, HDP>, cudaFuncAttributeMaxDynamicSharedMemorySize, ApLayout<HDP>::SMEM); })) return e;
     k_attn_prompt<T, HDP><<<grid, AP_THREADS, ApLayout<HDP>::SMEM, st>>>(mq, mk, mv, a);
     return cudaGetLastError();
 }

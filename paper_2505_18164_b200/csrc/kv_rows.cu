@@ -8,8 +8,8 @@
 // product are rounded.  The remainder x - k * scale is exact in one fma (|k| <= 127, and near a border it is a multiple of the
 // operands' last place no larger than scale / 2), so comparing it with scale / 2 puts k right.
 //
-// Bound: bytes.  A block takes `rpb` rows of the call; one thread per row finds its sequence (binary search), slot, page; then
-// groups of head_dim / 8 lanes take one row of one head each, 16 bytes a lane where the type is 16-bit, UN rows in flight.
+// Bound: bytes.  A block takes `rpb` rows of the call; a warp per row finds its sequence, slot and page; then
+// groups of head_dim / 8 lanes take one row of one head each, 16 bytes a lane where the type is 16-bit, UN rows in flight.  Read back of e4m3 as bf16 moves 5.4 TB/s (0.84 of the measured copy).
 #include "ops_common.cuh"
 
 #include <cuda_fp8.h>
@@ -21,7 +21,7 @@ namespace {
 
 constexpr int KR_THREADS = 256;
 constexpr int KR_MAX_RPB = 64; // rows per block
-constexpr int KR_UN = 4;       // rows in flight per lane group
+constexpr int KR_UN = 2;       // rows of a head in flight per lane group (4: read back of 4 x 32768 rows 10% slower, 8: 40%)
 
 struct KrArgs {
     OpCache c;
@@ -32,14 +32,13 @@ struct KrArgs {
     unsigned units_magic;          // ceil(2^32 / units): u / units = mulhi(u, magic) for the small u of a block
 };
 
-// Where row `row` of the call lives: index of (page, row in page) as page * page_tokens + row, or -1.
-__device__ __forceinline__ void kr_place(const KrArgs &a, int row, bool read, long long &page, int &at) {
+// Where row `row` of the call, one of sequence i if of any, lives: page and row in the page.
+__device__ __forceinline__ void kr_place(const KrArgs &a, int row, int i, bool read, long long &page, int &at) {
     page = -1;
     at = -1; // -1: nothing to do, -2 (read only): zeros
     if (row >= a.n_rows) return;
     const int total = a.start[a.n_seq];
     if (row >= total) return;
-    const int i = op_find(a.start, a.n_seq, row);
     const int first = a.start[i], next = a.start[i + 1];
     if (i == 0 && row < first) return;
     if (row < first || row >= next) { op_status(a.status, MDI_STATUS_RANGE); return; }
@@ -133,7 +132,10 @@ __global__ void __launch_bounds__(KR_THREADS) k_kv_rows(const KrArgs a) {
     __shared__ long long s_page[KR_MAX_RPB];
     __shared__ int s_at[KR_MAX_RPB];
     const int row0 = blockIdx.x * a.rpb, tid = threadIdx.x, sub = tid % LPR, grp = tid / LPR;
-    if (tid < a.rpb) kr_place(a, row0 + tid, READ, s_page[tid], s_at[tid]);
+    for (int r = tid >> 5; r < a.rpb; r += KR_THREADS / 32) { // a warp per row: its sequence is found 32 at a time
+        const int i = op_find_warp(a.start, a.n_seq, row0 + r, tid & 31);
+        if ((tid & 31) == 0) kr_place(a, row0 + r, i, READ, s_page[r], s_at[r]);
+    }
     __syncthreads();
     const int n_units = min(a.rpb, a.n_rows - row0) * a.units;
     for (int u0 = blockIdx.y * GROUPS * KR_UN; u0 < n_units; u0 += gridDim.y * GROUPS * KR_UN) {
@@ -235,10 +237,14 @@ int kr_call(const char *who, bool read, const mdi_kv_cache *cache, int n_seq, co
     a.n_seq = n_seq; a.n_rows = n_rows;
     a.units = 2 * cache->n_kv_head;
     a.units_magic = (unsigned)(((1ull << 32) + a.units - 1) / a.units);
-    // a block's share: about one round of its lane groups, UN rows each
+    // A block's share: rounds of its lane groups, UN rows each.  Finding a row's place takes a chain of dependent loads, so where
+    // there is work for every SM several times over a block takes more rows (4 x 32768 rows of 8 x 128: 1, 2, 4 rounds 168, 155,
+    // 150 us); where there is not, fewer, and there are more blocks (64 rows of 32 x 128: 7.4, 7.6, 11 us).
     const int groups = KR_THREADS / (cache->head_dim / 8) * KR_UN;
-    a.rpb = std::max(1, std::min(KR_MAX_RPB, groups / a.units));
-    const dim3 grid((n_rows + a.rpb - 1) / a.rpb, std::max(1, std::min(64, (a.rpb * a.units + groups - 1) / groups)));
+    const int64_t passes = (int64_t)n_rows * a.units / groups;
+    const int rounds = passes >= 4 * 148 * 8 ? 4 : passes >= 148 * 8 ? 2 : 1;
+    a.rpb = std::max(1, std::min(KR_MAX_RPB, groups * rounds / a.units));
+    const dim3 grid((n_rows + a.rpb - 1) / a.rpb, std::max(1, std::min(64, (a.rpb * a.units + groups * rounds - 1) / (groups * rounds))));
     cudaStream_t st = (cudaStream_t)stream;
 #define KR_GO(ST)                                                                  \
     do {                                                                           \

@@ -69,6 +69,12 @@ struct Partition {
     uint16_t *pf_hi = nullptr, *pf_lo = nullptr;
     float *pf_qkv = nullptr, *pf_q = nullptr, *pf_o = nullptr, *pf_h = nullptr, *pf_u = nullptr, *pf_xa = nullptr, *pf_xb = nullptr,
           *pf_part = nullptr; // split-K partial sums [PF_SPLIT_MAX][PF_CHUNK][d_model]
+    // 8-bit cache: scales of its rows, what the attention operators want to know of a call (KqMeta), the one-token attention's
+    // workspace, and for first visits queries, outputs and the rows cached so far as fp16
+    float *kv_scale = nullptr;
+    KqMeta *kq_meta = nullptr;
+    uint8_t *kq_ws = nullptr;
+    __half *kq_q = nullptr, *kq_o = nullptr, *kq_k = nullptr, *kq_v = nullptr;
     int64_t weight_bytes = 0, buffer_bytes = 0;
 };
 
@@ -87,6 +93,7 @@ struct mdi_ctx {
     size_t page_elems = 0, esize = 2, kv_esize = 4;
     bool kv_f32 = true;
     int kv_kind = 0; // KV_F32 / KV_BF16 / KV_F16
+    int kq_dtype = 0; // MDI_KV_I8 / MDI_KV_E4M3, 0: not an 8-bit cache (kv_kind then has no meaning)
     std::vector<Partition> part;
     std::vector<LayerW> layer;
     void *wte = nullptr, *wpe = nullptr, *lm_head = nullptr;
@@ -454,6 +461,48 @@ int enqueue_partition_step(mdi_ctx *c, int p, const Batch &bt, const float *x_in
 constexpr int PF_CHUNK = 128; // positions per pass through a partition (one tile of positions per GEMM block)
 constexpr int PF_SPLIT_MAX = 8; // K splits of the GEMMs with few row tiles (output projection, MLP down)
 
+// One layer's part of an 8-bit cache as the attention operators see it.
+mdi_kv_cache kq_cache(const mdi_ctx *c, const Partition &P, int layer_local) {
+    mdi_kv_cache k{};
+    k.pool_dev = P.kv_pool; k.scale_dev = P.kv_scale;
+    k.page_table_dev = P.pt_dev + (size_t)layer_local * c->pages_per_seq;
+    k.page_table_stride = (int64_t)(P.hi - P.lo) * c->pages_per_seq;
+    k.n_pages = P.n_pages; k.n_slots = c->S; k.pages_per_seq = c->pages_per_seq; k.page_tokens = c->page_tokens;
+    k.n_kv_head = c->s.n_kv_head; k.head_dim = c->s.head_dim; k.dtype = c->kq_dtype;
+    return k;
+}
+
+// Attention of one layer over an 8-bit cache, from the projection's rows P.pf_qkv to the bf16 planes of the output projection's input:
+// rotary embedding, append, then for a group's step (bt) the one-token attention, for T new positions of a first visit whose rows
+// before have been cached (`first` of them) the rows read back as fp16 and the prompt attention over them.
+int kq_attention(mdi_ctx *c, Partition &P, int layer_local, const Batch *bt, int slot, int first, int T, int ysl, __nv_bfloat16 *hi, __nv_bfloat16 *lo, cudaStream_t st) {
+    const mdi_model_shape &s = c->s;
+    const int qw = s.n_head * s.head_dim, kw = s.n_kv_head * s.head_dim, rows = qw + 2 * kw;
+    const float scale = 1.0f / std::sqrt((float)s.head_dim);
+    const mdi_kv_cache kc = kq_cache(c, P, layer_local);
+    KqMeta *m = P.kq_meta;
+    launch_k(c->pdl, k_kq_prepare, dim3(T, ysl), dim3(256), 0, st, P.pf_qkv, qw, kw, s.head_dim, (int)(s.arch == MDI_ARCH_LLAMA), (const float *)c->rope_cos,
+             (const float *)c->rope_sin, (const int *)P.pos_dev, slot, bt ? *bt : Batch{}, T, m, bt ? (__half *)nullptr : P.kq_q);
+    const mdi_rows k{P.pf_qkv + qw, MDI_DTYPE_F32, rows, s.head_dim}, v{P.pf_qkv + qw + kw, MDI_DTYPE_F32, rows, s.head_dim};
+    int rc = mdi_kv_append(&kc, bt ? T : 1, m->slot, m->start, m->pos, T, &k, &v, &m->status, st);
+    if (rc == MDI_OK && bt) {
+        const mdi_rows q{P.pf_qkv, MDI_DTYPE_F32, rows, s.head_dim}, o{P.obuf, MDI_DTYPE_F32, qw, s.head_dim};
+        rc = mdi_attn_decode(&kc, T, m->slot, m->len, s.n_ctx, s.n_head, &q, &o, scale, P.kq_ws, mdi_attn_decode_workspace(&kc, T, s.n_head, s.n_ctx), &m->status, st);
+        launch_k(c->pdl, k_pf_norm_split, dim3(T, ysl), dim3(PF_THREADS), 0, st, (const float *)P.obuf, qw, (int)NORM_NONE, (const float *)nullptr,
+                 (const float *)nullptr, 0.f, hi, lo, (const float *)nullptr, 0, T, (const float *)nullptr, (float *)nullptr);
+        c->st.kernel_launches += c->capturing ? 0 : 5;
+        if (c->capturing) c->cap_launches += 5;
+    } else if (rc == MDI_OK) {
+        const mdi_rows kd{P.kq_k, MDI_DTYPE_F16, kw, s.head_dim}, vd{P.kq_v, MDI_DTYPE_F16, kw, s.head_dim};
+        const mdi_rows q{P.kq_q, MDI_DTYPE_F16, qw, s.head_dim}, o{P.kq_o, MDI_DTYPE_F16, qw, s.head_dim};
+        rc = mdi_kv_read(&kc, 1, m->slot, m->all, nullptr, first + T, &kd, &vd, &m->status, st);
+        if (rc == MDI_OK) rc = mdi_attn_prompt(1, m->start, m->all, T, first + T, s.n_head, s.n_kv_head, s.head_dim, &q, &kd, &vd, &o, scale, &m->status, st);
+        launch_k(c->pdl, k_kq_split, dim3(T, ysl), dim3(256), 0, st, (const __half *)P.kq_o, qw, hi, lo);
+        c->st.kernel_launches += 5;
+    }
+    return rc == MDI_OK ? rc : fail(c, rc, "%s", g_create_error.c_str());
+}
+
 int pf_setup(mdi_ctx *c) {
     const mdi_model_shape &s = c->s;
     c->pf_tc = s.weight_dtype == MDI_DTYPE_BF16 && c->o.prefill_mode != 1;
@@ -464,6 +513,7 @@ int pf_setup(mdi_ctx *c) {
         const int d = s.d_model, qw = s.n_head * s.head_dim, kw = s.n_kv_head * s.head_dim;
         const double layer_bytes = 2.0 * ((double)(qw + 2 * kw) * d + (double)d * qw + (double)(s.act == MDI_ACT_SWIGLU ? 3 : 2) * s.d_ff * d);
         c->tc_min_group = c->o.tc_min_group > 0 ? c->o.tc_min_group : (layer_bytes >= 48e6 ? 1 : 5);
+        if (c->kq_dtype) c->tc_min_group = 1; // only that path knows an 8-bit cache
     }
     if (!c->pf_tc) return MDI_OK;
     CU(cudaFuncSetAttribute(k_tc_gemm, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TG_SMEM));
@@ -482,6 +532,17 @@ int pf_setup(mdi_ctx *c) {
         if ((rc = dalloc(c, &P.pf_xa, (size_t)PF_CHUNK * d, &P.buffer_bytes)) != MDI_OK) return rc;
         if ((rc = dalloc(c, &P.pf_xb, (size_t)PF_CHUNK * d, &P.buffer_bytes)) != MDI_OK) return rc;
         if ((rc = dalloc(c, &P.pf_part, (size_t)PF_SPLIT_MAX * PF_CHUNK * d, &P.buffer_bytes)) != MDI_OK) return rc;
+        if (!c->kq_dtype) continue;
+        const int kw = s.n_kv_head * s.head_dim;
+        if ((rc = dalloc(c, &P.kq_meta, 1, &P.buffer_bytes)) != MDI_OK) return rc;
+        if ((rc = dalloc(c, &P.kq_q, (size_t)PF_CHUNK * qw, &P.buffer_bytes)) != MDI_OK) return rc;
+        if ((rc = dalloc(c, &P.kq_o, (size_t)PF_CHUNK * qw, &P.buffer_bytes)) != MDI_OK) return rc;
+        if ((rc = dalloc(c, &P.kq_k, (size_t)s.n_ctx * kw, &P.buffer_bytes)) != MDI_OK) return rc;
+        if ((rc = dalloc(c, &P.kq_v, (size_t)s.n_ctx * kw, &P.buffer_bytes)) != MDI_OK) return rc;
+        const mdi_kv_cache kc = kq_cache(c, P, 0);
+        const int64_t ws = mdi_attn_decode_workspace(&kc, MAXB, s.n_head, s.n_ctx);
+        if (ws < 0) return fail(c, (int)ws, "%s", g_create_error.c_str());
+        if ((rc = dalloc(c, &P.kq_ws, (size_t)ws, &P.buffer_bytes)) != MDI_OK) return rc;
     }
     return MDI_OK;
 }
@@ -549,12 +610,13 @@ template <typename KT> void pf_attn_hd(bool pdl, int hd, dim3 g, cudaStream_t st
 }
 
 // The blocks of partition p on T rows with the linear layers on the tensor cores.  Two uses:
-//  - first visit (bt == null): T (<= PF_CHUNK) consecutive new positions of `slot`; partition 0 embeds tok_dev[0..T);
+//  - first visit (bt == null): T (<= PF_CHUNK) consecutive new positions of `slot` behind `first` earlier ones; partition 0 embeds
+//    tok_dev[0..T);
 //  - a group's decode step (bt != null): T = bt->n items of different slots, one new position each.
 // x_in: [T][d] (ignored for partition 0 of a first visit); x_out: [T][d].  Cache rows are appended and the
 // positions advanced at the end.  Per block: norm+split, QKV GEMM, rotary+append, attention (writes bf16 planes),
 // output-projection GEMM, norm+split (adds up split-K partials), MLP up GEMM (writes bf16 planes), MLP down GEMM.
-int tc_layers(mdi_ctx *c, int p, const Batch *bt, int slot, const int *tok_dev, int T, const float *x_in, float *x_out, cudaStream_t st) {
+int tc_layers(mdi_ctx *c, int p, const Batch *bt, int slot, int first, const int *tok_dev, int T, const float *x_in, float *x_out, cudaStream_t st) {
     Partition &P = c->part[p];
     const mdi_model_shape &s = c->s;
     const int d = s.d_model, F = s.d_ff, qw = s.n_head * s.head_dim, kw = s.n_kv_head * s.head_dim;
@@ -583,7 +645,9 @@ int tc_layers(mdi_ctx *c, int p, const Batch *bt, int slot, const int *tok_dev, 
         count_launch(c);
         pend = PfPending();
         if ((rc = pf_gemm(c, P, L.wqkv, qw + 2 * kw, d, T, L.bqkv, nullptr, TG_NONE, P.pf_qkv, nullptr, nullptr, nullptr, st)) != MDI_OK) return rc;
-        if (bt) {
+        if (c->kq_dtype) {
+            if ((rc = kq_attention(c, P, ll, bt, slot, first, T, ysl, hi, lo, st)) != MDI_OK) return rc;
+        } else if (bt) {
             KV_DISPATCH(c->kv_kind, launch_k(pdl, k_bt_rope_append<KT>, dim3(T, ysl), dim3(256), 0, st, P.pf_qkv, qw, kw, s.head_dim, rope, c->rope_cos, c->rope_sin, kv, ll, P.pos_dev, *bt, P.qbuf));
             count_launch(c);
             AttnArgs a{};
@@ -658,14 +722,14 @@ int tc_head(mdi_ctx *c, const Batch &hb, const float *x_rows, const HeadReq &hea
     return MDI_OK;
 }
 
-int pf_partition_chunk(mdi_ctx *c, int p, int slot, const int *tok_dev, int T, const float *x_in, float *x_out, cudaStream_t st) {
-    const int rc = tc_layers(c, p, nullptr, slot, tok_dev, T, x_in, x_out, st);
+int pf_partition_chunk(mdi_ctx *c, int p, int slot, int first, const int *tok_dev, int T, const float *x_in, float *x_out, cudaStream_t st) {
+    const int rc = tc_layers(c, p, nullptr, slot, first, tok_dev, T, x_in, x_out, st);
     if (rc == MDI_OK) ++c->st.stage_steps;
     return rc;
 }
 
 int tc_partition_step(mdi_ctx *c, int p, const Batch &bt, const float *x_in, float *x_out, cudaStream_t st) {
-    return tc_layers(c, p, &bt, 0, nullptr, bt.n, x_in, x_out, st);
+    return tc_layers(c, p, &bt, 0, 0, nullptr, bt.n, x_in, x_out, st);
 }
 
 // Did a tensor-core first visit give up on one of its bounded waits?  (Synchronises the partition streams.)
@@ -677,6 +741,13 @@ int pf_check(mdi_ctx *c) {
     if (e) {
         CU(cudaMemset(c->tg_err, 0, sizeof(int)));
         return fail(c, MDI_ERR_TIMEOUT, "a tensor-core first-visit kernel gave up waiting for its operands");
+    }
+    for (auto &P : c->part) {
+        if (!P.kq_meta) continue;
+        CU(cudaMemcpy(&e, &P.kq_meta->status, sizeof(int), cudaMemcpyDeviceToHost));
+        if (!e) continue;
+        CU(cudaMemset(&P.kq_meta->status, 0, sizeof(int)));
+        return fail(c, e & MDI_STATUS_TIMEOUT ? MDI_ERR_TIMEOUT : MDI_ERR_STATE, "attention over the 8-bit cache reported status %d", e);
     }
     return MDI_OK;
 }
@@ -771,6 +842,7 @@ int pk_setup(mdi_ctx *c) {
     cudaDeviceProp prop;
     CU(cudaGetDeviceProperties(&prop, c->dev));
     c->n_sm = prop.multiProcessorCount;
+    if (c->kq_dtype) return MDI_OK; // the stream scheduler's
     if (c->scheduler == 1 || c->scheduler == 3 || c->scheduler == 4) return MDI_OK;
     const bool want = c->scheduler == 2;
     if (c->gmax > PK_MAXNB) return want ? fail(c, MDI_ERR_SHAPE, "persistent scheduler: at most %d samples per group", PK_MAXNB) : MDI_OK;
@@ -979,7 +1051,7 @@ int fz_setup(mdi_ctx *c) {
     const bool want = c->scheduler == 3;
     auto no = [&](const char *why) { return want ? fail(c, MDI_ERR_SHAPE, "fused-phase scheduler: %s", why) : MDI_OK; };
     if (c->scheduler == 1 || c->scheduler == 2 || c->scheduler == 4) return MDI_OK;
-    if (s.arch != MDI_ARCH_GPT || s.weight_dtype != MDI_DTYPE_BF16 || !c->kv_f32) return no("needs the GPT block, bf16 weights and an fp32 cache");
+    if (s.arch != MDI_ARCH_GPT || s.weight_dtype != MDI_DTYPE_BF16 || !c->kv_f32 || c->kq_dtype) return no("needs the GPT block, bf16 weights and an fp32 cache");
     if (s.n_kv_head != H || H * hd != d) return no("needs n_kv_head = n_head and n_head * head_dim = d_model");
     if (d % 16 || s.d_ff % 16 || hd % 16) return no("widths must be multiples of 16");
     if (d > FZ_U * FZ_CTHREADS) return no("d_model above 1024");
@@ -1684,7 +1756,8 @@ void mdi_destroy(mdi_ctx *c) {
     }
     for (auto &P : c->part) {
         void *ptrs[] = {P.kv_pool, P.pt_dev, P.pos_dev, P.x_embed, P.qbuf, P.obuf, P.hbuf, P.part, P.x_last, P.attn_ticket,
-                        P.ring, P.pf_buf[0], P.pf_buf[1], P.pf_hi, P.pf_lo, P.pf_qkv, P.pf_q, P.pf_o, P.pf_h, P.pf_u, P.pf_xa, P.pf_xb, P.pf_part};
+                        P.ring, P.pf_buf[0], P.pf_buf[1], P.pf_hi, P.pf_lo, P.pf_qkv, P.pf_q, P.pf_o, P.pf_h, P.pf_u, P.pf_xa, P.pf_xb, P.pf_part,
+                        P.kv_scale, P.kq_meta, P.kq_ws, P.kq_q, P.kq_o, P.kq_k, P.kq_v};
         for (void *q : ptrs) if (q) cudaFree(q);
         for (auto e : P.ev_edge) cudaEventDestroy(e);
         for (auto e : P.ev_edge_cap) cudaEventDestroy(e);
@@ -1751,14 +1824,22 @@ int mdi_create(const mdi_model_shape *shape, const int *part_bounds, int K, int 
         // ... and 64 rows where the tensor-core persistent kernel may run (a warp hands out the page-table entries of
         // its sequence split by shuffles: fewer, larger pages)
         const bool td_candidate = s.weight_dtype == MDI_DTYPE_BF16 && c->o.scheduler == 4;
-        c->page_tokens = c->o.page_tokens > 0 ? c->o.page_tokens : (fused_candidate ? 128 : td_candidate ? 64 : 16);
+        const bool kq = c->o.kv_cache_dtype == MDI_KV_I8 || c->o.kv_cache_dtype == MDI_KV_E4M3; // 64 rows: a page-table entry per two tiles of 32
+        c->page_tokens = c->o.page_tokens > 0 ? c->o.page_tokens : (fused_candidate ? 128 : td_candidate || kq ? 64 : 16);
     }
     if (c->page_tokens & (c->page_tokens - 1)) return bail(fail(c, MDI_ERR_ARG, "page_tokens must be a power of two"));
     c->page_shift = 0;
     while ((1 << c->page_shift) < c->page_tokens) ++c->page_shift;
     c->pages_per_seq = (s.n_ctx + c->page_tokens - 1) / c->page_tokens;
     c->esize = s.weight_dtype == MDI_DTYPE_F32 ? 4 : 2;
-    if (c->o.kv_cache_dtype < 0 || c->o.kv_cache_dtype > 3) return bail(fail(c, MDI_ERR_ARG, "kv_cache_dtype must be one of MDI_KV_*"));
+    if (c->o.kv_cache_dtype < 0 || c->o.kv_cache_dtype > MDI_KV_E4M3) return bail(fail(c, MDI_ERR_ARG, "kv_cache_dtype must be one of MDI_KV_*"));
+    if (c->o.kv_cache_dtype == MDI_KV_I8 || c->o.kv_cache_dtype == MDI_KV_E4M3) {
+        if (s.weight_dtype != MDI_DTYPE_BF16 || c->o.prefill_mode != 0) return bail(fail(c, MDI_ERR_SHAPE, "an 8-bit cache needs bf16 weights and prefill_mode 0"));
+        if (c->o.scheduler > 1) return bail(fail(c, MDI_ERR_SHAPE, "an 8-bit cache runs on the stream scheduler (0 or 1)"));
+        if (c->page_tokens < 16) return bail(fail(c, MDI_ERR_SHAPE, "an 8-bit cache needs pages of at least 16 rows"));
+        if (s.n_kv_head > 1024 || s.n_head / s.n_kv_head > 64) return bail(fail(c, MDI_ERR_SHAPE, "an 8-bit cache takes at most 1024 key/value heads, 64 heads each"));
+        c->kq_dtype = c->o.kv_cache_dtype;
+    }
     {
         // default: fp16 for bf16 models outside the fused-phase kernel's reach (that kernel reads fp32 pages), else fp32
         const bool fused_shape = s.arch == MDI_ARCH_GPT && s.n_kv_head == s.n_head && s.d_model <= 1024 && s.head_dim <= 64;
@@ -1766,7 +1847,7 @@ int mdi_create(const mdi_model_shape *shape, const int *part_bounds, int K, int 
         c->kv_kind = s.weight_dtype != MDI_DTYPE_BF16 ? KV_F32 : want == MDI_KV_BF16 ? KV_BF16 : want == MDI_KV_F16 ? KV_F16 : KV_F32;
     }
     c->kv_f32 = c->kv_kind == KV_F32;
-    c->kv_esize = c->kv_f32 ? 4 : 2;
+    c->kv_esize = c->kq_dtype ? 1 : c->kv_f32 ? 4 : 2;
     c->page_elems = (size_t)2 * s.n_kv_head * c->page_tokens * s.head_dim;
     c->n_split = c->o.attn_splits > 0 ? c->o.attn_splits : std::max(1, std::min(16, s.n_ctx / 128));
     c->rounds_per_graph = c->o.rounds_per_graph != 0 ? c->o.rounds_per_graph : 16;
@@ -1852,6 +1933,7 @@ int mdi_create(const mdi_model_shape *shape, const int *part_bounds, int K, int 
         P.kv_bytes = (size_t)P.n_pages * c->page_elems * c->kv_esize;
         CUB(cudaMalloc(&P.kv_pool, std::max<size_t>(P.kv_bytes, 16)));
         CUB(cudaMemset(P.kv_pool, 0, std::max<size_t>(P.kv_bytes, 16)));
+        if (c->kq_dtype) TRY(dalloc(c, &P.kv_scale, (size_t)P.n_pages * 2 * s.n_kv_head * c->page_tokens, &P.buffer_bytes));
         P.free_pages.resize(P.n_pages);
         for (int i = 0; i < P.n_pages; ++i) P.free_pages[i] = P.n_pages - 1 - i;
         P.pt_host.assign((size_t)n_samples * Lp * c->pages_per_seq, 0);
@@ -2010,7 +2092,7 @@ static int prefill_impl(mdi_ctx *c, int sample, const int32_t *prompt, int n, bo
             const int m = std::min(PF_CHUNK, n - c0);
             const float *x_in = p > 0 ? c->part[p - 1].pf_buf[par] + (size_t)c0 * d : nullptr;
             float *x_out = p < K - 1 ? P.pf_buf[par] + (size_t)c0 * d : P.pf_xb;
-            if ((rc = pf_partition_chunk(c, p, sample, pbuf + c0, m, x_in, x_out, P.stream)) != MDI_OK) return rc;
+            if ((rc = pf_partition_chunk(c, p, sample, c0, pbuf + c0, m, x_in, x_out, P.stream)) != MDI_OK) return rc;
             if (p == K - 1 && c0 + m == n) {
                 Batch hb{};
                 hb.n = 1; hb.slot[0] = sample;

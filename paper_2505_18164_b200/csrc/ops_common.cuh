@@ -6,6 +6,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
+#include <atomic>
 #include <initializer_list>
 #include <stdint.h>
 
@@ -23,6 +24,19 @@ int op_check_ptrs(const char *who, std::initializer_list<OpPtr> ptrs);
 int op_check_rows(const char *who, const char *name, const mdi_rows *r, int rows, int heads);
 int op_check_cache(const char *who, const mdi_kv_cache *c);
 inline bool op_scaled(const mdi_kv_cache *c) { return c->dtype == MDI_KV_I8 || c->dtype == MDI_KV_E4M3; }
+
+// Runs a call once per device and place of use (setting a kernel's shared memory costs as much as its launch).
+struct OpOnce {
+    std::atomic<uint64_t> done{0}; // a bit per device
+    template <typename F> cudaError_t operator()(F f) {
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e != cudaSuccess) return e;
+        if (dev < 64 && (done.load(std::memory_order_acquire) >> dev & 1)) return cudaSuccess;
+        if ((e = f()) == cudaSuccess && dev < 64) done.fetch_or(1ull << dev, std::memory_order_release);
+        return e;
+    }
+};
 
 // ---- device view of a paged cache ------------------------------------------------------------------------------
 struct OpCache {
@@ -50,16 +64,19 @@ __device__ __forceinline__ int op_slot(const OpCache &c, int i) {
     const int s = c.slot ? c.slot[i] : i;
     return (unsigned)s < (unsigned)c.n_slots ? s : -1;
 }
-// last sequence i of [0, n_seq) with start[i] <= row (start ascends; the caller checks start[i] <= row < start[i + 1])
-__device__ __forceinline__ int op_find(const int *start, int n_seq, int row) {
-    int lo = 0, hi = n_seq - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (start[mid] <= row) lo = mid; else hi = mid - 1;
+// Last sequence i of [0, n_seq) with start[i] <= row (start ascends; the caller checks start[i] <= row < start[i + 1]).  All lanes of
+// a warp: each round looks at 32 places at once, so that up to 1024 sequences take two dependent loads.
+__device__ __forceinline__ int op_find_warp(const int *start, int n_seq, int row, int lane) {
+    int lo = 0, n = n_seq;
+    while (n > 1) {
+        const int step = (n + 31) / 32, i = lane * step;
+        const unsigned at = __ballot_sync(0xffffffffu, i < n && start[lo + min(i, n - 1)] <= row);
+        const int k = at ? 31 - __clz(at) : 0;
+        lo += k * step;
+        n = min(step, n - k * step);
     }
     return lo;
 }
-
 // ---- 8 elements of a row ---------------------------------------------------------------------------------------
 struct F8 { float v[8]; };
 

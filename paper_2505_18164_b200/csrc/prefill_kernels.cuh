@@ -283,6 +283,63 @@ __global__ void k_bt_rope_append(const float *qkv, int q_rows, int kv_rows, int 
     }
 }
 
+// ---- around the attention operators on an 8-bit cache (their own arguments, in device memory)
+struct KqMeta {
+    int slot[MAXB], pos[MAXB], len[MAXB]; // of each sequence of the call: page-table row, position of its first new row, rows with the new one
+    int start[MAXB + 1];                  // its first new row in the packed rows
+    int all[2];                           // first visit: where all of its rows, cached ones included, begin and end
+    int status;                           // MDI_STATUS_* bits
+};
+
+// Rotary embedding of q and k in place in the projection's rows qkv[t][q | k | v], with the queries also as fp16 where q16 is given;
+// block (0, 0) describes the call: a first visit's T positions of `slot` (bt.n = 0), or a step of bt.n items.  grid (T, row slices)
+__global__ void k_kq_prepare(float *qkv, int q_rows, int kv_rows, int hd, int rope, const float *rope_cos, const float *rope_sin, const int *pos,
+                             int slot, Batch bt, int T, KqMeta *m, __half *q16) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const int t = blockIdx.x, half = hd >> 1, p = bt.n ? pos[bt.slot[t]] + bt.off[t] : pos[slot] + t;
+    float *row = qkv + (size_t)t * (q_rows + 2 * kv_rows);
+    for (int r = blockIdx.y * blockDim.x + threadIdx.x; r < (q_rows + kv_rows) / 2; r += gridDim.y * blockDim.x) {
+        const int i = r % half, e = r / half * hd + i; // elements e and e + half of a head
+        float a = row[e], b = row[e + half];
+        if (rope) {
+            const float c = rope_cos[(size_t)p * half + i], s = rope_sin[(size_t)p * half + i];
+            const float ra = a * c - b * s, rb = b * c + a * s;
+            row[e] = a = ra;
+            row[e + half] = b = rb;
+        }
+        if (q16 && e < q_rows) {
+            q16[(size_t)t * q_rows + e] = __float2half_rn(a);
+            q16[(size_t)t * q_rows + e + half] = __float2half_rn(b);
+        }
+    }
+    if (blockIdx.x == 0 && blockIdx.y == 0) {
+        const int i = threadIdx.x;
+        if (bt.n) {
+            if (i < bt.n) {
+                m->slot[i] = bt.slot[i];
+                m->pos[i] = pos[bt.slot[i]] + bt.off[i];
+                m->len[i] = m->pos[i] + 1;
+            }
+            if (i <= bt.n) m->start[i] = i;
+        } else if (i == 0) {
+            m->slot[0] = slot;
+            m->pos[0] = p;
+            m->start[0] = m->all[0] = 0;
+            m->start[1] = T;
+            m->all[1] = p + T;
+        }
+    }
+}
+
+// fp16 rows as two bf16 planes (exact).  grid (T, column slices)
+__global__ void k_kq_split(const __half *x, int n, __nv_bfloat16 *hi, __nv_bfloat16 *lo) {
+    pdl_launch_dependents();
+    pdl_wait();
+    for (int i = blockIdx.y * blockDim.x + threadIdx.x; i < n; i += gridDim.y * blockDim.x)
+        pf_split_store(hi, lo, (size_t)blockIdx.x * n + i, __half2float(x[(size_t)blockIdx.x * n + i]));
+}
+
 __global__ void k_bt_advance(int *pos, Batch bt) {
     pdl_launch_dependents();
     pdl_wait();

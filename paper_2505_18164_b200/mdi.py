@@ -134,7 +134,11 @@ def greedy_argmax_static(logits_dev, n_rows: int, n_cols: int, out_dev, stream: 
 
 # ---- operators on the caller's device tensors (see the second half of mdi.h) ------------------------------------------
 _ROW_DTYPES = {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2}
+_ROW_CODES: dict = {}  # the same by the dtype objects met so far (their names are slow to look up)
 _KV_DTYPES = {"torch.bfloat16": KV_BF16, "torch.float16": KV_F16, "torch.int8": KV_I8, "torch.float8_e4m3fn": KV_E4M3}
+
+
+_INT32: set = set()
 
 
 def _fail_arg(text: str):
@@ -148,11 +152,15 @@ def _op_check(rc: int):
 
 def _rows(name: str, t, rows: int, heads: int, head_dim: int) -> Rows:
     """A [rows][heads][head_dim] tensor (any strides but the last) as the library's row view."""
-    dt = _ROW_DTYPES.get(str(t.dtype))
+    dtype, shape = t.dtype, t.shape
+    dt = _ROW_CODES.get(dtype)
     if dt is None:
-        _fail_arg(f"{name}: dtype {t.dtype} is none of float32, bfloat16, float16")
-    if t.dim() != 3 or t.shape[0] < rows or t.shape[1] != heads or t.shape[2] != head_dim:
-        _fail_arg(f"{name}: shape {tuple(t.shape)}, expected [{rows}][{heads}][{head_dim}]")
+        dt = _ROW_DTYPES.get(str(dtype))
+        if dt is None:
+            _fail_arg(f"{name}: dtype {dtype} is none of float32, bfloat16, float16")
+        _ROW_CODES[dtype] = dt
+    if len(shape) != 3 or shape[0] < rows or shape[1] != heads or shape[2] != head_dim:
+        _fail_arg(f"{name}: shape {tuple(shape)}, expected [{rows}][{heads}][{head_dim}]")
     s0, s1, s2 = t.stride()
     if s2 != 1:
         _fail_arg(f"{name}: the elements of a head must be contiguous")
@@ -163,8 +171,9 @@ def _ints(name: str, t, n: int):
     """Address of a device tensor of at least n int32 values (None: 0)."""
     if t is None:
         return 0
-    if str(t.dtype) != "torch.int32" or t.numel() < n or not t.is_contiguous():
+    if t.dtype not in _INT32 and str(t.dtype) != "torch.int32" or t.numel() < n or not t.is_contiguous():
         _fail_arg(f"{name}: expected a contiguous int32 tensor of at least {n} elements")
+    _INT32.add(t.dtype)
     return t.data_ptr()
 
 
