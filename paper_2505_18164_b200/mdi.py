@@ -150,15 +150,20 @@ def _op_check(rc: int):
         raise MdiError(rc, (lib().mdi_last_error(None) or b"").decode())
 
 
+def _row_code(name: str, dtype) -> int:
+    dt = _ROW_DTYPES.get(str(dtype))
+    if dt is None:
+        _fail_arg(f"{name}: dtype {dtype} is none of float32, bfloat16, float16")
+    _ROW_CODES[dtype] = dt
+    return dt
+
+
 def _rows(name: str, t, rows: int, heads: int, head_dim: int) -> Rows:
     """A [rows][heads][head_dim] tensor (any strides but the last) as the library's row view."""
     dtype, shape = t.dtype, t.shape
     dt = _ROW_CODES.get(dtype)
     if dt is None:
-        dt = _ROW_DTYPES.get(str(dtype))
-        if dt is None:
-            _fail_arg(f"{name}: dtype {dtype} is none of float32, bfloat16, float16")
-        _ROW_CODES[dtype] = dt
+        dt = _row_code(name, dtype)
     if len(shape) != 3 or shape[0] < rows or shape[1] != heads or shape[2] != head_dim:
         _fail_arg(f"{name}: shape {tuple(shape)}, expected [{rows}][{heads}][{head_dim}]")
     s0, s1, s2 = t.stride()
@@ -171,9 +176,13 @@ def _ints(name: str, t, n: int):
     """Address of a device tensor of at least n int32 values (None: 0)."""
     if t is None:
         return 0
-    if t.dtype not in _INT32 and str(t.dtype) != "torch.int32" or t.numel() < n or not t.is_contiguous():
-        _fail_arg(f"{name}: expected a contiguous int32 tensor of at least {n} elements")
-    _INT32.add(t.dtype)
+    dtype = t.dtype
+    if dtype not in _INT32:
+        if str(dtype) != "torch.int32":
+            _fail_arg(f"{name}: expected int32, not {dtype}")
+        _INT32.add(dtype)
+    if t.numel() < n or not t.is_contiguous():
+        _fail_arg(f"{name}: expected a contiguous tensor of at least {n} elements")
     return t.data_ptr()
 
 
@@ -195,6 +204,7 @@ class KvCache:
             _fail_arg("scale: 8-bit caches need a contiguous float32 [n_pages][2][n_kv_head][page_tokens] tensor")
         self.tensors = (pool, page_table, scale)
         self.n_slots, self.n_kv_head, self.head_dim = page_table.shape[0], pool.shape[2], pool.shape[4]
+        self._lib = lib()
         self._c = KvCacheStruct(pool.data_ptr(), _ptr(scale) if scale is not None else 0, page_table.data_ptr(),
                                 page_table.stride(0) if self.n_slots > 1 else max(page_table.shape[1], 1), pool.shape[0], self.n_slots, page_table.shape[1], pool.shape[3],
                                 self.n_kv_head, self.head_dim, dt)
@@ -205,16 +215,16 @@ def kv_append(cache: KvCache, k, v, seq_start, pos, slots=None, status=None, str
     of sequence i's slot (``slots[i]``, or i)."""
     n_seq, n = seq_start.numel() - 1, k.shape[0]
     kr, vr = _rows("k", k, n, cache.n_kv_head, cache.head_dim), _rows("v", v, n, cache.n_kv_head, cache.head_dim)
-    _op_check(lib().mdi_kv_append(cache._c, n_seq, _ints("slots", slots, n_seq), _ints("seq_start", seq_start, n_seq + 1),
-                                  _ints("pos", pos, n_seq), n, kr, vr, _ints("status", status, 1), stream))
+    _op_check(cache._lib.mdi_kv_append(cache._c, n_seq, _ints("slots", slots, n_seq) if slots is not None else 0, _ints("seq_start", seq_start, n_seq + 1),
+                                  _ints("pos", pos, n_seq), n, kr, vr, _ints("status", status, 1) if status is not None else 0, stream))
 
 
 def kv_read(cache: KvCache, k_out, v_out, seq_start, pos=None, slots=None, status=None, stream: int = 0):
     """mdi_kv_read: the reverse of kv_append, into ``k_out``, ``v_out``; ``pos`` None reads every sequence from position 0."""
     n_seq, n = seq_start.numel() - 1, k_out.shape[0]
     kr, vr = _rows("k_out", k_out, n, cache.n_kv_head, cache.head_dim), _rows("v_out", v_out, n, cache.n_kv_head, cache.head_dim)
-    _op_check(lib().mdi_kv_read(cache._c, n_seq, _ints("slots", slots, n_seq), _ints("seq_start", seq_start, n_seq + 1),
-                                _ints("pos", pos, n_seq), n, kr, vr, _ints("status", status, 1), stream))
+    _op_check(cache._lib.mdi_kv_read(cache._c, n_seq, _ints("slots", slots, n_seq) if slots is not None else 0, _ints("seq_start", seq_start, n_seq + 1),
+                                _ints("pos", pos, n_seq), n, kr, vr, _ints("status", status, 1) if status is not None else 0, stream))
 
 
 def attn_decode_workspace(cache: KvCache, n_head: int, max_len: int = 0, n_seq: Optional[int] = None) -> int:
@@ -232,8 +242,8 @@ def attn_decode(cache: KvCache, q, out, lens, max_len: int = 0, scale: Optional[
     n_seq, n_head = q.shape[0], q.shape[1]
     qr, orow = _rows("q", q, n_seq, n_head, cache.head_dim), _rows("out", out, n_seq, n_head, cache.head_dim)
     ws = (workspace.data_ptr(), workspace.numel() * workspace.element_size()) if workspace is not None else (0, 0)
-    _op_check(lib().mdi_attn_decode(cache._c, n_seq, _ints("slots", slots, n_seq), _ints("lens", lens, n_seq), max_len, n_head, qr, orow,
-                                    cache.head_dim ** -0.5 if scale is None else scale, ws[0], ws[1], _ints("status", status, 1), stream))
+    _op_check(cache._lib.mdi_attn_decode(cache._c, n_seq, _ints("slots", slots, n_seq) if slots is not None else 0, _ints("lens", lens, n_seq), max_len, n_head, qr, orow,
+                                    cache.head_dim ** -0.5 if scale is None else scale, ws[0], ws[1], _ints("status", status, 1) if status is not None else 0, stream))
 
 
 def attn_prompt(q, k, v, out, q_start, k_start, scale: Optional[float] = None, status=None, stream: int = 0):
@@ -242,7 +252,7 @@ def attn_prompt(q, k, v, out, q_start, k_start, scale: Optional[float] = None, s
     n_seq, (nq, n_head, hd), (nk, n_kv) = q_start.numel() - 1, q.shape, k.shape[:2]
     r = [_rows("q", q, nq, n_head, hd), _rows("k", k, nk, n_kv, hd), _rows("v", v, nk, n_kv, hd), _rows("out", out, nq, n_head, hd)]
     _op_check(lib().mdi_attn_prompt(n_seq, _ints("q_start", q_start, n_seq + 1), _ints("k_start", k_start, n_seq + 1), nq, nk, n_head, n_kv, hd,
-                                    r[0], r[1], r[2], r[3], hd ** -0.5 if scale is None else scale, _ints("status", status, 1), stream))
+                                    r[0], r[1], r[2], r[3], hd ** -0.5 if scale is None else scale, _ints("status", status, 1) if status is not None else 0, stream))
 
 
 class Context:
