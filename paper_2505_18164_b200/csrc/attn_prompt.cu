@@ -268,6 +268,10 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     const uint32_t b_qfull = tg_smem_u32(&sh->qfull), b_full = tg_smem_u32(sh->full), b_empty = tg_smem_u32(sh->empty), b_s = tg_smem_u32(sh->sready),
                    b_p = tg_smem_u32(sh->pready), b_pv = tg_smem_u32(sh->pvdone), b_free = tg_smem_u32(&sh->sfree);
     if (warp == 0) ap_find_tile(a, blockIdx.x / a.n_head, lane, sh);
+    if (warp == 17) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tg_smem_u32(&sh->tmem)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
     if (tid == 32) {
         ap_init(b_qfull, 1);
         for (int i = 0; i < NST; ++i) { ap_init(b_full + 8 * i, 1); ap_init(b_empty + 8 * i, 1); }
@@ -279,26 +283,21 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         sh->poison = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
-    if (sh->tile < 0) return; // no such tile
-    const int row0 = sh->tile * 2 * AP_ROWS, nq = sh->nq, nk = sh->nk, q0 = sh->q0, k0 = sh->k0, off = nk - nq;
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const int row0 = max(sh->tile, 0) * 2 * AP_ROWS, nq = sh->tile < 0 ? 0 : sh->nq, // (without a tile: no rows, and nothing to do below)
+               nk = sh->nk, q0 = sh->q0, k0 = sh->k0, off = nk - nq;
     const int head = blockIdx.x % a.n_head, kvh = head / a.group;
     // key tiles of each sub-tile: up to what its last row sees
     int nt[2];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-        const int r0 = row0 + s * AP_ROWS, seen = r0 < nq ? min(nk, off + min(r0 + AP_ROWS, nq)) : 0;
+        const int r0 = row0 + s * AP_ROWS, seen = nq > 0 && r0 < nq ? min(nk, off + min(r0 + AP_ROWS, nq)) : 0;
         nt[s] = seen > 0 ? (seen + AP_ROWS - 1) / AP_ROWS : 0;
     }
     const int n_tiles = max(nt[0], nt[1]);
     const int masked_from = min(max(off + row0 + 1, 0), nk) / AP_ROWS; // first tile with a key that some row of the block does not see
-    if (warp == 17) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tg_smem_u32(&sh->tmem)), "r"(512) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    }
-    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-    __syncthreads();
-    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = sh->tmem;
     int *abort = &sh->abort;
 
@@ -532,6 +531,11 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             ap_meet(9 + s, 256); // the sums; and all of this sub-tile's looks at the values are done
             ok = ok && ap_wait_warp(b_pv + 8 * s, (n_mine - 1) & 1, abort, a.status);
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            // through shared memory (the sub-tile's queries are no longer needed there), so that stores cover whole lines: a row per
+            // thread, 16 bytes at a time, took 2000 clocks more
+            constexpr int CH = HDP / 16, LINE = CH * 16; // 16-byte chunks and bytes of this half of a row
+            unsigned char *mine = smem + L::Q + s * L::TILE + (warp & 7) * 32 * LINE;
+            auto swizzle = [](int r) { return CH == 8 ? r & 7 : (r >> 1) & 3; };
             const bool poison = *(volatile int *)&sh->poison;
             const float inv = seen > 0 ? 1.f / (sh->row[s][0][r] + sh->row[s][1][r]) : 0.f;
 #pragma unroll 1
@@ -555,18 +559,22 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                                 }
                             }
                 }
-                if (valid) {
 #pragma unroll
-                    for (int e = 0; e < 32; e += 8)
-                        if (o + e < a.hd) {
-                            uint4 w;
-                            w.x = ap_pack<T>(__uint_as_float(y[e]), __uint_as_float(y[e + 1]));
-                            w.y = ap_pack<T>(__uint_as_float(y[e + 2]), __uint_as_float(y[e + 3]));
-                            w.z = ap_pack<T>(__uint_as_float(y[e + 4]), __uint_as_float(y[e + 5]));
-                            w.w = ap_pack<T>(__uint_as_float(y[e + 6]), __uint_as_float(y[e + 7]));
-                            *(uint4 *)(out + o + e) = w;
-                        }
+                for (int e = 0; e < 32; e += 8) {
+                    uint4 w;
+                    w.x = ap_pack<T>(__uint_as_float(y[e]), __uint_as_float(y[e + 1]));
+                    w.y = ap_pack<T>(__uint_as_float(y[e + 2]), __uint_as_float(y[e + 3]));
+                    w.z = ap_pack<T>(__uint_as_float(y[e + 4]), __uint_as_float(y[e + 5]));
+                    w.w = ap_pack<T>(__uint_as_float(y[e + 6]), __uint_as_float(y[e + 7]));
+                    *(uint4 *)(mine + lane * LINE + (((o - half * (HDP / 2) + e) / 8 ^ swizzle(lane)) * 16)) = w;
                 }
+            }
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < CH; ++i) { // 32 rows of CH chunks, neighbouring lanes on a row
+                const int x = i * 32 + lane, rr = x / CH, ch = x % CH, col = half * (HDP / 2) + ch * 8, to = row - lane + rr;
+                if (ok && to < nq && col < a.hd)
+                    *(uint4 *)(out + (long long)(rr - lane) * a.out.row_stride + col) = *(const uint4 *)(mine + rr * LINE + ((ch ^ swizzle(rr)) * 16));
             }
         }
     }
