@@ -4,7 +4,10 @@
 // Bound: the tensor cores (4 head_dim flops per query, head and key seen) and, at head_dim 64 and close behind at 128, the
 // exponentials (one per query, head and key, 16 a clock and SM).
 //
-// One block takes 256 query rows of one head (two sub-tiles of 128) and walks the keys its rows see in tiles of 128, once:
+// A block per SM takes items one after the other: 256 query rows of one head (two sub-tiles of 128), whose keys it walks in tiles of
+// 128, once.  Its warps have their own loops over the items, so that loads and products of the next item run while the outputs of
+// the last one are still being written (a block per item spends 9000 clocks on filling and emptying itself, three tiles' worth):
+//   warp 19     looks items up, ahead of the others;
 //   warp 16     requests the tiles by TMA (128-byte swizzle, no multicast): queries once, then keys and values through one ring;
 //   warps 17, 18 issue tcgen05.mma, accumulators in tensor memory: one the scores S = Q K^T (128 x 128), the other the outputs O += P V.
 //               Both sub-tiles share one S: it is in use only until the softmax has taken the scores into registers, and the next
@@ -35,6 +38,7 @@ namespace {
 
 constexpr int AP_ROWS = 128;              // rows of a sub-tile, keys of a tile
 constexpr int AP_THREADS = 640;
+constexpr int AP_SM = 148;                // blocks: one per SM
 constexpr int AP_SORT = 64;               // up to this many sequences their tiles are taken in order of the keys they see
 constexpr unsigned long long AP_WAIT_NS = 2000000000ull;
 
@@ -49,20 +53,26 @@ struct ApArgs {
 
 template <int HDP> struct ApLayout {
     static constexpr int TILE = AP_ROWS * HDP * 2;
-    static constexpr int STAGES = HDP == 128 ? 5 : 8;
+    static constexpr int STAGES = HDP == 128 ? 4 : 8;
     // columns of tensor memory: scores, weights of sub-tile s at P + 64 s, outputs at O + HDP s
     static constexpr int P = 128, O = 256;
-    static constexpr int Q = 0, RING = 2 * TILE, BARS = RING + STAGES * TILE;
+    static constexpr int Q = 0, RING = 2 * TILE, OUT = RING + STAGES * TILE, BARS = OUT + 16 * 2048; // OUT: 2 KB per softmax warp
     static constexpr int SMEM = BARS + 2560; // barriers and what threads tell each other
 };
 
+struct ApItem { int tile, q0, nq, k0, nk, head, kvh; }; // a tile (negative: no more items), its sequence, its head and key/value head
 struct ApShared { // behind the ring
-    unsigned long long qfull, full[8], empty[8], sready[2], sfree, pready[4], pvdone[2], drain[2];
+    unsigned long long qfull, qempty, full[8], empty[8], sready[2], sfree, pready[4], pvdone[2], ofree[2], ifull[2], iempty[2], drain[2];
     unsigned tmem;
-    int abort, poison;
+    int abort, poison[4];          // poison: items (number + 1, by number mod 4) with values that had to be replaced
+    ApItem item[2];
     float row[2][2][AP_ROWS];      // [sub-tile][half][row]: what the two threads of a row tell each other
-    int tile, q0, nq, k0, nk; // this block's tile (negative: none) and its sequence
 };
+// key tiles of sub-tile s of an item: up to what its last row sees
+__device__ __forceinline__ int ap_key_tiles(const ApItem *i, int s) {
+    const int r0 = (2 * i->tile + s) * AP_ROWS, seen = i->tile >= 0 && r0 < i->nq ? min(i->nk, i->nk - i->nq + min(r0 + AP_ROWS, i->nq)) : 0;
+    return seen > 0 ? (seen + AP_ROWS - 1) / AP_ROWS : 0;
+}
 static_assert(sizeof(ApShared) <= 2560, "ApShared");
 
 __device__ __forceinline__ void ap_init(uint32_t bar, int n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(n) : "memory"); }
@@ -90,9 +100,6 @@ template <bool SLEEP> __device__ __noinline__ bool ap_wait_slow(uint32_t bar, ui
     op_status(status, MDI_STATUS_TIMEOUT);
     return false;
 }
-__device__ __forceinline__ bool ap_wait(uint32_t bar, uint32_t parity, int *abort, int *status) {
-    return tg_try_wait(bar, parity) || ap_wait_slow<true>(bar, parity, abort, status);
-}
 __device__ __forceinline__ void ap_tma(uint32_t dst, const CUtensorMap *map, int c0, int c1, int c2, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                  ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(bar) : "memory");
@@ -111,10 +118,10 @@ template <bool SLEEP = true> __device__ __forceinline__ bool ap_wait_warp(uint32
 }
 // named barriers of the softmax warps
 __device__ __forceinline__ void ap_meet(int bar, int threads) { asm volatile("barrier.cta.sync %0, %1;" ::"r"(bar), "r"(threads) : "memory"); }
-__device__ __forceinline__ bool ap_vote(int bar, bool yes) { // of 64 threads
+__device__ __forceinline__ bool ap_vote(int bar, bool yes, int threads) { // does any of them say yes?
     int any;
-    asm volatile("{\n .reg .pred p, q;\n setp.ne.b32 q, %1, 0;\n barrier.cta.red.or.pred p, %2, 64, q;\n selp.b32 %0, 1, 0, p;\n}\n"
-                 : "=r"(any) : "r"((int)yes), "r"(bar) : "memory");
+    asm volatile("{\n .reg .pred p, q;\n setp.ne.b32 q, %1, 0;\n barrier.cta.red.or.pred p, %2, %3, q;\n selp.b32 %0, 1, 0, p;\n}\n"
+                 : "=r"(any) : "r"((int)yes), "r"(bar), "r"(threads) : "memory");
     return any != 0;
 }
 // Shared-memory descriptors.  Queries and keys: rows of 128 bytes along head_dim, 128-byte swizzle, 8 rows = 1024 bytes.  Values: the
@@ -186,7 +193,7 @@ template <typename T> __device__ __forceinline__ uint32_t ap_nonfinite(uint32_t 
     return std::is_same<T, __half>::value ? ((w & 0x7c007c00u) + 0x04000400u) & 0x80008000u : ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
 }
 
-// Sequence and 256-row tile of the block, x-th in the order in which tiles are taken.  One warp.  A sequence whose offsets do not
+// Sequence and 256-row tile of an item, x-th in the order in which tiles are taken.  One warp.  A sequence whose offsets do not
 // fit has no tiles.  Tiles that see the most keys come first, so that no long one is left to run alone at the end: over all
 // sequences where there are at most AP_SORT (found by bisection on the number of key tiles), else sequence by sequence.
 struct ApSeq { int q0, nq, k0, nk, tiles; };
@@ -219,12 +226,11 @@ __device__ __forceinline__ int ap_scan(int n, int lane) { // sum over the lanes 
     }
     return n;
 }
-__device__ __forceinline__ void ap_found(ApShared *sh, const ApSeq &s, int tile) {
-    sh->tile = tile; sh->q0 = s.q0; sh->nq = s.nq; sh->k0 = s.k0; sh->nk = s.nk;
+__device__ __forceinline__ void ap_found(ApItem *it, const ApSeq &s, int tile) {
+    it->tile = tile; it->q0 = s.q0; it->nq = s.nq; it->k0 = s.k0; it->nk = s.nk;
 }
-__device__ __forceinline__ void ap_find_tile(const ApArgs &a, int x, int lane, ApShared *sh) {
-    const bool tell = blockIdx.x == 0;
-    if (lane == 0) sh->tile = -1;
+__device__ __forceinline__ void ap_find_tile(const ApArgs &a, int x, int lane, bool tell, ApItem *it) {
+    if (lane == 0) it->tile = -1;
     __syncwarp();
     if (a.n_seq <= AP_SORT) {
         const ApSeq s0 = ap_seq(a, lane, tell), s1 = ap_seq(a, lane + 32, tell);
@@ -237,8 +243,8 @@ __device__ __forceinline__ void ap_find_tile(const ApArgs &a, int x, int lane, A
         const int a0 = ap_at_least(s0, lo), a1 = ap_at_least(s1, lo), n0 = a0 - ap_at_least(s0, lo + 1), n1 = a1 - ap_at_least(s1, lo + 1);
         const int rank = x - (ap_sum(a0 + a1) - ap_sum(n0 + n1)); // among the tiles of exactly this level
         const int before = ap_scan(n0 + n1, lane) - n0 - n1;
-        if (rank >= before && rank < before + n0) ap_found(sh, s0, s0.tiles - a0 + rank - before);
-        else if (rank >= before + n0 && rank < before + n0 + n1) ap_found(sh, s1, s1.tiles - a1 + rank - before - n0);
+        if (rank >= before && rank < before + n0) ap_found(it, s0, s0.tiles - a0 + rank - before);
+        else if (rank >= before + n0 && rank < before + n0 + n1) ap_found(it, s1, s1.tiles - a1 + rank - before - n0);
     } else {
         long long total = 0;
         for (int b = 0; b < a.n_seq; b += 32) total += ap_sum(ap_seq(a, b + lane, tell).tiles);
@@ -248,16 +254,28 @@ __device__ __forceinline__ void ap_find_tile(const ApArgs &a, int x, int lane, A
             const ApSeq s = ap_seq(a, b + lane, false);
             const int incl = ap_scan(s.tiles, lane);
             const long long lo = before + incl - s.tiles;
-            if (lo <= at && at < lo + s.tiles) ap_found(sh, s, (int)(at - lo));
+            if (lo <= at && at < lo + s.tiles) ap_found(it, s, (int)(at - lo));
             before += __shfl_sync(0xffffffffu, incl, 31);
         }
     }
 }
 
-// grid: tiles x heads, the heads of a tile next to each other
+// The infinities and NaN among the values of key rows j0 .. j1 - 1 in columns o .. o + 31, added to a row's staged outputs.
+template <typename T> __device__ __noinline__ void ap_add_nonfinite(const ApArgs &a, unsigned char *line, int swizzle, int kvh, int j0, int j1, int o) {
+    const unsigned short *v = (const unsigned short *)a.v.data + kvh * a.v.head_stride + o;
+    for (int j = j0; j < j1; ++j)
+        for (int e = 0; e < 32 && o + e < a.hd; ++e) {
+            const unsigned short w = v[j * a.v.row_stride + e];
+            if (!(ap_nonfinite<T>(w) & 0x8000u)) continue;
+            T x, *y = (T *)(line + ((e / 8 ^ swizzle) * 16)) + e % 8;
+            *(unsigned short *)&x = w;
+            *y = (T)((float)*y + (float)x);
+        }
+}
+
 template <typename T, int HDP>
 __global__ void __launch_bounds__(AP_THREADS, 1)
-k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const ApArgs a) {
+k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ ApArgs a) {
     using L = ApLayout<HDP>;
     constexpr bool BF = std::is_same<T, __nv_bfloat16>::value;
     constexpr int NST = L::STAGES;
@@ -266,8 +284,8 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     const uint32_t s_base = tg_smem_u32(smem);
     const uint32_t b_qfull = tg_smem_u32(&sh->qfull), b_full = tg_smem_u32(sh->full), b_empty = tg_smem_u32(sh->empty), b_s = tg_smem_u32(sh->sready),
-                   b_p = tg_smem_u32(sh->pready), b_pv = tg_smem_u32(sh->pvdone), b_free = tg_smem_u32(&sh->sfree);
-    if (warp == 0) ap_find_tile(a, blockIdx.x / a.n_head, lane, sh);
+                   b_p = tg_smem_u32(sh->pready), b_pv = tg_smem_u32(sh->pvdone), b_free = tg_smem_u32(&sh->sfree),
+                   b_qempty = tg_smem_u32(&sh->qempty), b_ofree = tg_smem_u32(sh->ofree), b_ifull = tg_smem_u32(sh->ifull), b_iempty = tg_smem_u32(sh->iempty);
     if (warp == 17) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tg_smem_u32(&sh->tmem)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -277,63 +295,93 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         for (int i = 0; i < NST; ++i) { ap_init(b_full + 8 * i, 1); ap_init(b_empty + 8 * i, 1); }
         for (int i = 0; i < 2; ++i) { ap_init(b_s + 8 * i, 1); ap_init(b_pv + 8 * i, 1); }
         ap_init(b_free, 8);
+        ap_init(b_qempty, 1);
+        for (int i = 0; i < 2; ++i) { ap_init(b_ofree + 8 * i, 8); ap_init(b_ifull + 8 * i, 1); ap_init(b_iempty + 8 * i, 19); } // 16 softmax warps, TMA, two MMA
         for (int i = 0; i < 2; ++i) ap_init(tg_smem_u32(&sh->drain[i]), 1);
         for (int i = 0; i < 4; ++i) ap_init(b_p + 8 * i, 8); // sub-tile 0 first and second step, sub-tile 1
         sh->abort = 0;
-        sh->poison = 0;
+        for (int i = 0; i < 4; ++i) sh->poison[i] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    const int row0 = max(sh->tile, 0) * 2 * AP_ROWS, nq = sh->tile < 0 ? 0 : sh->nq, // (without a tile: no rows, and nothing to do below)
-               nk = sh->nk, q0 = sh->q0, k0 = sh->k0, off = nk - nq;
-    const int head = blockIdx.x % a.n_head, kvh = head / a.group;
-    // key tiles of each sub-tile: up to what its last row sees
-    int nt[2];
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-        const int r0 = row0 + s * AP_ROWS, seen = nq > 0 && r0 < nq ? min(nk, off + min(r0 + AP_ROWS, nq)) : 0;
-        nt[s] = seen > 0 ? (seen + AP_ROWS - 1) / AP_ROWS : 0;
-    }
-    const int n_tiles = max(nt[0], nt[1]);
-    const int masked_from = min(max(off + row0 + 1, 0), nk) / AP_ROWS; // first tile with a key that some row of the block does not see
     const uint32_t tmem = sh->tmem;
     int *abort = &sh->abort;
+    // Every warp waits for an item, reads what it wants of it from shared memory and says when it has (the softmax warps at the item's
+    // end: what is held in registers meanwhile would be spilled, and with all this shared memory there is next to no first-level cache
+    // behind the spills).
+    auto arrived = [&](int it) { return ap_wait_warp(b_ifull + 8 * (it & 1), (it >> 1) & 1, abort, a.status); };
+    auto done_with = [&](int it) {
+        __syncwarp();
+        if (lane == 0) ap_arrive(b_iempty + 8 * (it & 1));
+    };
 
-    if (warp == 16) {
-        if (lane == 0 && n_tiles > 0) { // ---- TMA
-            ap_expect(b_qfull, ((nt[0] > 0) + (nt[1] > 0)) * L::TILE);
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-                if (nt[s] > 0) ap_load<HDP>(s_base + L::Q + s * L::TILE, &tm_q, a.q_swap, head, q0 + row0 + s * AP_ROWS, b_qfull);
-            int issued = 0;
-            for (int n = 0; n < 2 * n_tiles; ++n) {
-                const int st = n % NST;
-                if (n >= NST && !ap_wait(b_empty + 8 * st, ((n / NST) & 1) ^ 1, abort, a.status)) break;
-                ap_expect(b_full + 8 * st, L::TILE);
-                const uint32_t dst = s_base + L::RING + st * L::TILE;
-                const int row = k0 + (n >> 1) * AP_ROWS;
-                if (n & 1) ap_load<HDP>(dst, &tm_v, a.v_swap, kvh, row, b_full + 8 * st);
-                else ap_load<HDP>(dst, &tm_k, a.k_swap, kvh, row, b_full + 8 * st);
-                issued = n + 1;
-            }
-            if (*(volatile int *)abort) { // nothing may land in this memory after the block has gone
-                int mine = 0;
-                ap_wait(b_qfull, 0, &mine, a.status);
-                for (int n = max(0, issued - NST); n < issued; ++n) ap_wait(b_full + 8 * (n % NST), (n / NST) & 1, &mine, a.status);
-            }
+    if (warp == 19) { // ---- items: the blocks take them in turn, to and fro, so that each gets long and short ones alike
+        for (int it = 0;; ++it) {
+            if (it >= 2 && !ap_wait_warp(b_iempty + 8 * (it & 1), ((it >> 1) & 1) ^ 1, abort, a.status)) break;
+            const long long x = (long long)it * gridDim.x + (it & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+            ApItem *i = &sh->item[it & 1];
+            ap_find_tile(a, (int)min(x / a.n_head, (long long)0x7fffffff), lane, it == 0 && blockIdx.x == 0, i);
+            __syncwarp();
+            const bool last = i->tile < 0;
+            if (lane == 0) { i->head = (int)(x % a.n_head); i->kvh = i->head / a.group; ap_arrive(b_ifull + 8 * (it & 1)); }
+            if (__any_sync(0xffffffffu, last)) break;
         }
-    } else if (warp > 16) {
-        if (n_tiles > 0 && warp < 19) { // ---- MMA: the whole warp, see ap_mma_ss
-            const uint32_t fmt = (1u << 4) | (BF ? (1u << 7) | (1u << 10) : 0u) | ((uint32_t)(AP_ROWS >> 4) << 24);
-            const int nt0 = __shfl_sync(0xffffffffu, nt[0], 0), nt1 = __shfl_sync(0xffffffffu, nt[1], 0), n_all = max(nt0, nt1);
-            const uint32_t base = __shfl_sync(0xffffffffu, s_base, 0), td = __shfl_sync(0xffffffffu, tmem, 0);
+    } else if (warp == 16) { // ---- TMA (lane 0; the others only keep step)
+        int n = 0, items = 0; // tiles of keys and values requested so far, items with queries
+        for (int it = 0;; ++it) {
+            if (!arrived(it)) break;
+            const ApItem *i_ = &sh->item[it & 1];
+            const int nt0 = ap_key_tiles(i_, 0), nt1 = ap_key_tiles(i_, 1), n_tiles = max(nt0, nt1), kvh = i_->kvh, head = i_->head, k0 = i_->k0, q_row = i_->q0 + i_->tile * 2 * AP_ROWS;
+            const bool more = i_->tile >= 0;
+            done_with(it);
+            if (!more) break;
             bool ok = true;
-            if (warp == 17) { // scores
-                const uint32_t id_s = fmt | ((uint32_t)(AP_ROWS >> 3) << 17);
-                int st = 0, par = 0, uses = 0; // ring stage of the tile's keys and its parity; uses of S so far
-                ok = ap_wait_warp(b_qfull, 0, abort, a.status);
+            for (int i = 0; i < 2 * n_tiles && ok; ++i, ++n) {
+                const int st = n % NST;
+                if (n >= NST) ok = ap_wait_warp(b_empty + 8 * st, ((n / NST) & 1) ^ 1, abort, a.status);
+                if (!ok) break;
+                if (lane == 0) {
+                    ap_expect(b_full + 8 * st, L::TILE);
+                    const uint32_t dst = s_base + L::RING + st * L::TILE;
+                    const int row = k0 + (i >> 1) * AP_ROWS;
+                    if (i & 1) ap_load<HDP>(dst, &tm_v, a.v_swap, kvh, row, b_full + 8 * st);
+                    else ap_load<HDP>(dst, &tm_k, a.k_swap, kvh, row, b_full + 8 * st);
+                }
+                if (i == 0) { // the queries, once the previous item's are no longer needed
+                    if (items > 0) ok = ap_wait_warp(b_qempty, (items - 1) & 1, abort, a.status);
+                    if (ok && lane == 0) {
+                        ap_expect(b_qfull, ((nt0 > 0) + (nt1 > 0)) * L::TILE);
+                        if (nt0 > 0) ap_load<HDP>(s_base + L::Q, &tm_q, a.q_swap, head, q_row, b_qfull);
+                        if (nt1 > 0) ap_load<HDP>(s_base + L::Q + L::TILE, &tm_q, a.q_swap, head, q_row + AP_ROWS, b_qfull);
+                    }
+                    if (ok) ++items;
+                }
+            }
+            if (!ok) break;
+        }
+        if (*(volatile int *)abort) { // nothing may land in this memory after the block has gone
+            int mine = 0;
+            if (items > 0) ap_wait_warp(b_qfull, (items - 1) & 1, &mine, a.status);
+            for (int i = max(0, n - NST); i < n; ++i) ap_wait_warp(b_full + 8 * (i % NST), (i / NST) & 1, &mine, a.status);
+        }
+    } else if (warp > 16) { // ---- MMA: the whole warp, see ap_mma_ss
+        const uint32_t fmt = (1u << 4) | (BF ? (1u << 7) | (1u << 10) : 0u) | ((uint32_t)(AP_ROWS >> 4) << 24);
+        const uint32_t base = __shfl_sync(0xffffffffu, s_base, 0), td = __shfl_sync(0xffffffffu, tmem, 0);
+        bool ok = true;
+        if (warp == 17) { // scores
+            const uint32_t id_s = fmt | ((uint32_t)(AP_ROWS >> 3) << 17);
+            int st = 0, par = 0, uses = 0, items = 0; // ring stage of the tile's keys and its parity; uses of S so far; items with queries
+            for (int it = 0; ok; ++it) {
+                ok = arrived(it);
+                if (!ok) break;
+                const int nt0 = __shfl_sync(0xffffffffu, ap_key_tiles(&sh->item[it & 1], 0), 0), nt1 = __shfl_sync(0xffffffffu, ap_key_tiles(&sh->item[it & 1], 1), 0), n_all = max(nt0, nt1);
+                const bool last = __any_sync(0xffffffffu, sh->item[it & 1].tile < 0);
+                done_with(it);
+                if (last) break;
+                if (n_all == 0) continue;
+                ok = ap_wait_warp(b_qfull, items++ & 1, abort, a.status);
                 for (int j = 0; j < n_all && ok; ++j) {
                     ok = ap_wait_warp(b_full + 8 * st, par, abort, a.status);
                     const uint32_t k = base + L::RING + st * L::TILE;
@@ -357,19 +405,32 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                     st += 2;
                     if (st >= NST) { st -= NST; par ^= 1; }
                 }
-            } else { // outputs
-                const uint32_t id_o = fmt | (1u << 16) | ((uint32_t)(HDP >> 3) << 17);
-                int st = 1, par = 0;
+                if (ok) ap_commit(b_qempty);
+            }
+        } else { // outputs
+            const uint32_t id_o = fmt | (1u << 16) | ((uint32_t)(HDP >> 3) << 17);
+            int st = 1, par = 0, tiles[2] = {0, 0}, items[2] = {0, 0}; // of each sub-tile so far
+            for (int it = 0; ok; ++it) {
+                ok = arrived(it);
+                if (!ok) break;
+                const int nt0 = __shfl_sync(0xffffffffu, ap_key_tiles(&sh->item[it & 1], 0), 0), nt1 = __shfl_sync(0xffffffffu, ap_key_tiles(&sh->item[it & 1], 1), 0), n_all = max(nt0, nt1);
+                const bool last = __any_sync(0xffffffffu, sh->item[it & 1].tile < 0);
+                done_with(it);
+                if (last) break;
                 for (int j = 0; j < n_all && ok; ++j) {
                     ok = ap_wait_warp(b_full + 8 * st, par, abort, a.status);
                     const uint32_t v = base + L::RING + st * L::TILE;
 #pragma unroll
                     for (int s = 0; s < 2; ++s) {
                         if (j >= (s ? nt1 : nt0)) continue;
+                        if (j == 0) { // the outputs of the sub-tile's previous item have been taken
+                            if (items[s] > 0) ok = ok && ap_wait_warp<false>(b_ofree + 8 * s, (items[s] - 1) & 1, abort, a.status);
+                            ++items[s];
+                        }
                         // weights of the keys 0-31 and 64-95, then of the others
 #pragma unroll
                         for (int step = 0; step < 2; ++step) {
-                            ok = ok && ap_wait_warp<false>(b_p + 16 * s + 8 * step, j & 1, abort, a.status);
+                            ok = ok && ap_wait_warp<false>(b_p + 16 * s + 8 * step, tiles[s] & 1, abort, a.status);
                             if (!ok) break;
                             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
@@ -378,6 +439,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                                 ap_mma_ts(td + L::O + s * HDP, td + L::P + s * 64 + e * 8, ap_desc_mn(v + e * 2048), id_o, j > 0 || step > 0 || i > 0);
                             }
                         }
+                        ++tiles[s];
                         if (ok) ap_commit(b_pv + 8 * s);
                     }
                     if (!ok) break;
@@ -386,27 +448,35 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                     if (st >= NST) { st -= NST; par ^= 1; }
                 }
             }
-            if (!ok) { // no product may still run when the block goes
-                int mine = 0;
-                ap_commit(tg_smem_u32(&sh->drain[warp - 17]));
-                ap_wait_warp(tg_smem_u32(&sh->drain[warp - 17]), 0, &mine, a.status);
-            }
+        }
+        if (!ok) { // no product may still run when the block goes
+            int mine = 0;
+            ap_commit(tg_smem_u32(&sh->drain[warp - 17]));
+            ap_wait_warp(tg_smem_u32(&sh->drain[warp - 17]), 0, &mine, a.status);
         }
     } else {
         // ---- softmax: sub-tile s, half of the keys of a tile; thread = row = tensor memory lane
-        const int s = warp >> 3, half = (warp >> 2) & 1, r = (warp & 3) * 32 + lane, row = row0 + s * AP_ROWS + r; // row of the sequence
+        const int s = warp >> 3, half = (warp >> 2) & 1, r = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)(warp & 3) << 21, t_s = tmem + lanes + 64 * half, t_p = tmem + lanes + L::P + s * 64 + 32 * half, t_o = tmem + lanes + L::O + s * HDP;
         const int two = 1 + s * 4 + (warp & 3);  // named barrier of the two warps that share 32 rows
-        const int seen = min(off + row + 1, nk); // keys this row sees (also for rows behind the sequence: never stored)
-        const int n_mine = s ? nt[1] : nt[0];
-        const float c = a.scale_log2e;
-        float m = -INFINITY, l = 0.f; // what the weights refer to (in raw scores), sum of this thread's weights
-        bool ok = true;
-        for (int j = 0; j < n_mine; ++j) {
+        // Few registers are left beside a row's 64 scores: what can be read again from shared memory is.
+        int t = 0, ring = 1;                     // tiles of this sub-tile so far; place in the ring (counted on) of the values of the tile `t`
+        for (int it = 0;; ++it) {
+        bool ok = arrived(it);
+        const ApItem *item = &sh->item[it & 1];
+        if (ap_vote(9 + s, !ok, 256) || item->tile < 0) break; // all of the sub-tile's warps go on, or none
+        const int t_end = t + ap_key_tiles(item, s);
+        int here = min(item->nk - item->nq + (2 * item->tile + s) * AP_ROWS + r + 1, item->nk) - 64 * half; // keys of this half and on that the row sees
+        // first tile with a key that some row of the item does not see
+        const int t_masked = t + min(max(item->nk - item->nq + item->tile * 2 * AP_ROWS + 1, 0), item->nk) / AP_ROWS;
+        bool first = true;
+        float m = -INFINITY, l = 0.f; // what the weights refer to (in log2 units), sum of this thread's weights
+        for (; t < t_end; ++t, here -= AP_ROWS, ring += 2) {
             // (after a wait that ran out a warp goes on to meet its partner at the barriers, and does nothing else)
-            ok = ok && ap_wait_warp(b_s + 8 * s, j & 1, abort, a.status);
+            ok = ok && ap_wait_warp(b_s + 8 * s, t & 1, abort, a.status);
             if (!ok) {
-                if (ap_vote(two, false)) { ap_meet(two, 64); ap_meet(two, 64); }
+                if (ap_vote(two, false, 64)) { ap_meet(two, 64); ap_meet(two, 64); }
+                first = false;
                 continue;
             }
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -417,7 +487,6 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
             __syncwarp();
             if (lane == 0) ap_arrive(b_free); // S may hold the other sub-tile's scores
-            const int here = seen - j * AP_ROWS - 64 * half; // this half's keys that the row sees
             if (__any_sync(0xffffffffu, here < 64)) {
 #pragma unroll
                 for (int e = 0; e < 64; ++e)
@@ -435,17 +504,18 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             float top = ap_max_nan(ap_max_nan(t4[0], t4[1], t4[2]), t4[3], t4[3]);
             if (!(top < INFINITY)) l = __uint_as_float(0x7fc00000u); // a score of +inf or NaN: the row is NaN
             // does any row of the two warps need another reference?
-            const bool rise = m == -INFINITY ? top > -INFINITY : (top - m) * c > 8.f;
-            if (ap_vote(two, rise)) {
+            const float c = a.scale_log2e;
+            const bool rise = m == -INFINITY ? top > -INFINITY : top * c - m > 8.f;
+            if (ap_vote(two, rise, 64)) {
                 sh->row[s][half][r] = top;
                 ap_meet(two, 64);
                 const float other = sh->row[s][half ^ 1][r], high = fmaxf(top, other); // (a NaN is dropped: its row's sum is NaN already)
-                const bool up = m == -INFINITY ? high > -INFINITY : (high - m) * c > 8.f;
-                const float f = up ? (m == -INFINITY ? 0.f : ap_exp2((m - high) * c)) : 1.f;
-                if (up) m = high;
+                const bool up = m == -INFINITY ? high > -INFINITY : high * c - m > 8.f;
+                const float f = up ? (m == -INFINITY ? 0.f : ap_exp2(m - high * c)) : 1.f;
+                if (up) m = high * c;
                 l *= f;
-                if (j > 0) { // half of O's columns each, once the product of the previous tile is in
-                    ok = ap_wait_warp(b_pv + 8 * s, (j - 1) & 1, abort, a.status);
+                if (!first) { // half of O's columns each, once the product of the previous tile is in
+                    ok = ap_wait_warp(b_pv + 8 * s, (t - 1) & 1, abort, a.status);
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
                     for (int o = half * (HDP / 2); o < (half + 1) * (HDP / 2); o += 16) { // (16 at a time: the 64 scores are held meanwhile)
@@ -461,11 +531,11 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                 }
                 ap_meet(two, 64); // O is rescaled, and row[] may be written again
             }
-            if (j >= masked_from) { // values of this tile that may meet a weight of zero: infinities and NaN out (the 64 rows of this half)
-                const int nv = 2 * j + 1;
-                ok = ok && ap_wait_warp(b_full + 8 * (nv % NST), (nv / NST) & 1, abort, a.status);
+            first = false;
+            if (t >= t_masked) { // values of this tile that may meet a weight of zero: infinities and NaN out (the 64 rows of this half)
+                ok = ok && ap_wait_warp(b_full + 8 * (ring % NST), (ring / NST) & 1, abort, a.status);
                 if (!ok) continue;
-                unsigned char *v = smem + L::RING + (nv % NST) * L::TILE + (64 * half + (r >> 1)) * 128; // two threads a row
+                unsigned char *v = smem + L::RING + (ring % NST) * L::TILE + (64 * half + (r >> 1)) * 128; // two threads a row
                 constexpr int PART = HDP / 16; // 16-byte chunks each
                 const int c0 = (r & 1) * PART;
                 uint32_t bad = 0;
@@ -476,7 +546,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                     bad |= ap_nonfinite<T>(w.x) | ap_nonfinite<T>(w.y) | ap_nonfinite<T>(w.z) | ap_nonfinite<T>(w.w);
                 }
                 if (bad) {
-                    *(volatile int *)&sh->poison = 1;
+                    *(volatile int *)&sh->poison[it & 3] = it + 1;
                     __threadfence_block();
                     for (int q = c0 * 4; q < (c0 + PART) * 4; ++q) {
                         uint32_t *w = (uint32_t *)(v + (q >> 5) * (AP_ROWS * 128)) + (q & 31);
@@ -488,10 +558,10 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             }
             // The previous weights have been used.  (Waiting here rather than before the first store, half an exponential phase later,
             // keeps the sub-tiles out of step: 2990 instead of 3400 clocks a tile.)
-            ok = ok && (j == 0 || ap_wait_warp(b_pv + 8 * s, (j - 1) & 1, abort, a.status));
+            ok = ok && (t == 0 || ap_wait_warp(b_pv + 8 * s, (t - 1) & 1, abort, a.status));
             if (!ok) continue;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const float ref = m == -INFINITY ? 0.f : m * c;
+            const float ref = m == -INFINITY ? 0.f : m;
             const ap_f2 c2 = ap_pair(c, c), r2 = ap_pair(-ref, -ref);
             ap_f2 sum0 = ap_pair(0.f, 0.f), sum1 = sum0;
             // (Replacing a quarter of the exponentials by polynomials on the multiply-add pipe made a tile 20% slower: the exponential
@@ -520,23 +590,25 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                 l += s0 + s1;
             }
         }
+        const int n_mine = ap_key_tiles(item, s);
+        ring += 2 * (max(ap_key_tiles(item, 0), ap_key_tiles(item, 1)) - n_mine); // the other sub-tile's
         // ---- output: half of the columns each
+        const int seen = min(item->nk - item->nq + (2 * item->tile + s) * AP_ROWS + r + 1, item->nk);
+        const int row = (2 * item->tile + s) * AP_ROWS + r, nq = item->nq; // row of the sequence
         const bool valid = row < nq;
-        T *out = (T *)a.out.data + (long long)(q0 + row) * a.out.row_stride + (long long)head * a.out.head_stride;
+        T *out = (T *)a.out.data + (long long)(item->q0 + row) * a.out.row_stride + (long long)item->head * a.out.head_stride;
         if (n_mine == 0) {
             if (valid && half == 0)
                 for (int e = 0; e < a.hd; e += 8) *(uint4 *)(out + e) = make_uint4(0, 0, 0, 0);
         } else {
             sh->row[s][half][r] = l;
             ap_meet(9 + s, 256); // the sums; and all of this sub-tile's looks at the values are done
-            ok = ok && ap_wait_warp(b_pv + 8 * s, (n_mine - 1) & 1, abort, a.status);
+            ok = ok && ap_wait_warp(b_pv + 8 * s, (t - 1) & 1, abort, a.status);
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            // through shared memory (the sub-tile's queries are no longer needed there), so that stores cover whole lines: a row per
-            // thread, 16 bytes at a time, took 2000 clocks more
-            constexpr int CH = HDP / 16, LINE = CH * 16; // 16-byte chunks and bytes of this half of a row
-            unsigned char *mine = smem + L::Q + s * L::TILE + (warp & 7) * 32 * LINE;
-            auto swizzle = [](int r) { return CH == 8 ? r & 7 : (r >> 1) & 3; };
-            const bool poison = *(volatile int *)&sh->poison;
+            // 32 columns at a time through shared memory, so that stores cover whole sectors side by side: a row per thread, 16 bytes at a
+            // time, took 2000 clocks more
+            unsigned char *mine = smem + L::OUT + warp * 2048;
+            const bool poison = *(volatile int *)&sh->poison[it & 3] == it + 1;
             const float inv = seen > 0 ? 1.f / (sh->row[s][0][r] + sh->row[s][1][r]) : 0.f;
 #pragma unroll 1
             for (int o = half * (HDP / 2); o < (half + 1) * (HDP / 2) && ok; o += 32) {
@@ -545,20 +617,6 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                 ap_wait_ld();
 #pragma unroll
                 for (int e = 0; e < 32; ++e) y[e] = seen > 0 ? __float_as_uint(__uint_as_float(y[e]) * inv) : 0u;
-                if (poison && valid) {
-                    const unsigned short *v = (const unsigned short *)a.v.data + kvh * a.v.head_stride;
-                    for (int j = masked_from * AP_ROWS; j < seen; ++j)
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (o + e < a.hd) {
-                                const unsigned short w = v[(long long)(k0 + j) * a.v.row_stride + o + e];
-                                if (ap_nonfinite<T>(w) & 0x8000u) {
-                                    T t;
-                                    *(unsigned short *)&t = w;
-                                    y[e] = __float_as_uint(__uint_as_float(y[e]) + (float)t);
-                                }
-                            }
-                }
 #pragma unroll
                 for (int e = 0; e < 32; e += 8) {
                     uint4 w;
@@ -566,16 +624,25 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                     w.y = ap_pack<T>(__uint_as_float(y[e + 2]), __uint_as_float(y[e + 3]));
                     w.z = ap_pack<T>(__uint_as_float(y[e + 4]), __uint_as_float(y[e + 5]));
                     w.w = ap_pack<T>(__uint_as_float(y[e + 6]), __uint_as_float(y[e + 7]));
-                    *(uint4 *)(mine + lane * LINE + (((o - half * (HDP / 2) + e) / 8 ^ swizzle(lane)) * 16)) = w;
+                    *(uint4 *)(mine + lane * 64 + ((e / 8 ^ (lane >> 1 & 3)) * 16)) = w;
                 }
-            }
-            __syncwarp();
+                if (poison && valid) ap_add_nonfinite<T>(a, mine + lane * 64, lane >> 1 & 3, item->kvh, item->k0 + min(max(item->nk - item->nq + item->tile * 2 * AP_ROWS + 1, 0), item->nk) / AP_ROWS * AP_ROWS, item->k0 + seen, o);
+                if (o + 32 == (half + 1) * (HDP / 2)) { // the last of this warp's columns: the next item's outputs may come
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) ap_arrive(b_ofree + 8 * s);
+                }
+                __syncwarp();
 #pragma unroll
-            for (int i = 0; i < CH; ++i) { // 32 rows of CH chunks, neighbouring lanes on a row
-                const int x = i * 32 + lane, rr = x / CH, ch = x % CH, col = half * (HDP / 2) + ch * 8, to = row - lane + rr;
-                if (ok && to < nq && col < a.hd)
-                    *(uint4 *)(out + (long long)(rr - lane) * a.out.row_stride + col) = *(const uint4 *)(mine + rr * LINE + ((ch ^ swizzle(rr)) * 16));
+                for (int i = 0; i < 4; ++i) { // 32 rows of 4 chunks, four neighbouring lanes on a row
+                    const int rr = i * 8 + lane / 4, ch = lane & 3, col = o + ch * 8, to = row - lane + rr;
+                    if (to < nq && col < a.hd)
+                        *(uint4 *)(out + (long long)(rr - lane) * a.out.row_stride + col) = *(const uint4 *)(mine + rr * 64 + ((ch ^ (rr >> 1 & 3)) * 16));
+                }
+                __syncwarp();
             }
+        }
+        done_with(it);
         }
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -652,9 +719,8 @@ extern "C" int mdi_attn_prompt(int n_seq, const int32_t *q_start_dev, const int3
     a.q_start = q_start_dev; a.k_start = k_start_dev; a.status = status_dev;
     a.n_seq = n_seq; a.n_q = n_q_rows; a.n_k = n_k_rows; a.n_head = n_head; a.group = n_head / n_kv_head; a.hd = head_dim;
     a.scale_log2e = scale * 1.4426950408889634f;
-    const int64_t blocks = ((int64_t)n_q_rows / (2 * AP_ROWS) + std::min(n_seq, n_q_rows)) * n_head;
-    if (blocks > 0x7fffffff) return op_fail(MDI_ERR_SHAPE, "%s: too many rows and heads for one call", who);
-    const dim3 grid((unsigned)blocks);
+    const int64_t items = ((int64_t)n_q_rows / (2 * AP_ROWS) + std::min(n_seq, n_q_rows)) * n_head; // at most
+    const dim3 grid((unsigned)std::min<int64_t>(items, AP_SM));
     cudaStream_t st = (cudaStream_t)stream;
     cudaError_t ce;
     if (q->dtype == MDI_DTYPE_F16) ce = head_dim == 128 ? ap_launch<__half, 128>(mq, mk, mv, a, grid, st) : ap_launch<__half, 64>(mq, mk, mv, a, grid, st);
