@@ -132,8 +132,10 @@ template <int ST, int UPPER> __device__ __forceinline__ uint32_t ad_wide(uint32_
         const __half2 r = __hsub2(*(const __half2 *)&h, __half2half2(__ushort_as_half(0x6480))); // - 1152
         return *(const uint32_t *)&r;
     } else {
-        const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(UPPER ? w >> 16 : w & 0xffffu), __NV_E4M3);
-        return (uint32_t)r.x | (uint32_t)r.y << 16;
+        uint32_t r; // (the intrinsic works on 16-bit pieces, which cost a permutation each to take apart and to put together)
+        if constexpr (UPPER) asm("{\n .reg .b16 lo, hi;\n mov.b32 {lo, hi}, %1;\n cvt.rn.f16x2.e4m3x2 %0, hi;\n}\n" : "=r"(r) : "r"(w));
+        else asm("{\n .reg .b16 lo, hi;\n mov.b32 {lo, hi}, %1;\n cvt.rn.f16x2.e4m3x2 %0, lo;\n}\n" : "=r"(r) : "r"(w));
+        return r;
     }
 }
 template <int ST> __device__ __forceinline__ uint32_t ad_bias(uint32_t w) { return ST == AD_I8 ? w ^ 0x80808080u : w; }
