@@ -312,7 +312,7 @@ typedef struct {
 /* Write new rows into the cache (Section III-D: the cached matrices are extended).  k, v: packed rows of n_kv_head heads, any
  * dtype; rows seq_start_dev[i] .. seq_start_dev[i+1]-1 belong to sequence i of n_seq and go to positions pos_dev[i] and
  * following of its slot.  seq_start_dev: [n_seq+1]; n_rows: rows that k and v hold; rows at or behind
- * seq_start_dev[n_seq] are not read.  slot_dev: page-table row of each sequence, NULL: sequence i has slot i.
+ * seq_start_dev[n_seq] are ignored.  slot_dev: page-table row of each sequence, NULL: sequence i has slot i.
  * Two rows of one call must not go to the same place. */
 int mdi_kv_append(const mdi_kv_cache *cache, int n_seq, const int32_t *slot_dev, const int32_t *seq_start_dev, const int32_t *pos_dev,
                   int n_rows, const mdi_rows *k, const mdi_rows *v, int32_t *status_dev, void *stream);

@@ -116,8 +116,10 @@ template <> __device__ __forceinline__ F8 kr_unpack<StE4M3>(const StRaw<StE4M3> 
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const unsigned w = i < 2 ? r.a.x : r.a.y;
-        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> (16 * (i & 1))), __NV_E4M3);
-        const float2 x = __half22float2(__half2(h));
+        unsigned h;
+        if (i & 1) asm("{\n .reg .b16 lo, hi;\n mov.b32 {lo, hi}, %1;\n cvt.rn.f16x2.e4m3x2 %0, hi;\n}\n" : "=r"(h) : "r"(w));
+        else asm("{\n .reg .b16 lo, hi;\n mov.b32 {lo, hi}, %1;\n cvt.rn.f16x2.e4m3x2 %0, lo;\n}\n" : "=r"(h) : "r"(w));
+        const float2 x = __half22float2(*(const __half2 *)&h);
         f.v[2 * i] = x.x;
         f.v[2 * i + 1] = x.y;
     }
@@ -132,38 +134,55 @@ __global__ void __launch_bounds__(KR_THREADS) k_kv_rows(const KrArgs a) {
     __shared__ long long s_page[KR_MAX_RPB];
     __shared__ int s_at[KR_MAX_RPB];
     const int row0 = blockIdx.x * a.rpb, tid = threadIdx.x, sub = tid % LPR, grp = tid / LPR;
+    const int n_units = min(a.rpb, a.n_rows - row0) * a.units, first = blockIdx.y * GROUPS * KR_UN;
+    // unit u of the block: row of the block, keys or values, head
+    auto split = [&](int u, int &rl, int &which, int &h) {
+        rl = (int)__umulhi((unsigned)u, a.units_magic);
+        const int w = u - rl * a.units;
+        which = w >= a.c.n_kv_head;
+        h = w - (which ? a.c.n_kv_head : 0);
+    };
+    auto address = [&](int rl, int which, int h) {
+        const OpRows &t = which ? a.v : a.k;
+        return t.data + ((row0 + rl) * t.row_stride + h * t.head_stride + sub * 8) * (long long)sizeof(RT);
+    };
+    typename RowIO<RT>::Raw in[KR_UN]; // append: the rows of a round; of the first one while their places are looked up
+    auto fetch = [&](int u0) {
+#pragma unroll
+        for (int j = 0; j < KR_UN; ++j) {
+            const int u = u0 + j * GROUPS + grp;
+            int rl, which, h;
+            split(min(u, n_units - 1), rl, which, h);
+            if (u < n_units) in[j] = RowIO<RT>::load(address(rl, which, h));
+        }
+    };
+    if (!READ && first < n_units) fetch(first);
     for (int r = tid >> 5; r < a.rpb; r += KR_THREADS / 32) { // a warp per row: its sequence is found 32 at a time
         const int i = op_find_warp(a.start, a.n_seq, row0 + r, tid & 31);
         if ((tid & 31) == 0) kr_place(a, row0 + r, i, READ, s_page[r], s_at[r]);
     }
     __syncthreads();
-    const int n_units = min(a.rpb, a.n_rows - row0) * a.units;
-    for (int u0 = blockIdx.y * GROUPS * KR_UN; u0 < n_units; u0 += gridDim.y * GROUPS * KR_UN) {
-        long long src[KR_UN], dst[KR_UN]; // byte offset of the row in the tensor, index of the row in the pool (negative: see kr_place)
+    for (int u0 = first; u0 < n_units; u0 += gridDim.y * GROUPS * KR_UN) {
+        long long dst[KR_UN]; // index of the row in the pool (negative: see kr_place)
         unsigned char *base[KR_UN];
 #pragma unroll
         for (int j = 0; j < KR_UN; ++j) {
             const int u = u0 + j * GROUPS + grp;
             dst[j] = -1;
             if (u < n_units) {
-                const int rl = (int)__umulhi((unsigned)u, a.units_magic), w = u - rl * a.units;
-                const int which = w >= a.c.n_kv_head, h = w - (which ? a.c.n_kv_head : 0);
-                const OpRows &t = which ? a.v : a.k;
-                base[j] = t.data;
-                src[j] = ((row0 + rl) * t.row_stride + h * t.head_stride + sub * 8) * (long long)sizeof(RT);
+                int rl, which, h;
+                split(u, rl, which, h);
+                base[j] = address(rl, which, h);
                 const int at = s_at[rl];
                 dst[j] = at < 0 ? at : (((s_page[rl] * 2 + which) * a.c.n_kv_head + h) << a.c.page_shift) + at;
             }
         }
         if (!READ) {
-            typename RowIO<RT>::Raw raw[KR_UN];
-#pragma unroll
-            for (int j = 0; j < KR_UN; ++j)
-                if (dst[j] >= 0) raw[j] = RowIO<RT>::load(base[j] + src[j]);
+            if (u0 != first) fetch(u0);
 #pragma unroll
             for (int j = 0; j < KR_UN; ++j) {
                 F8 x{};
-                if (dst[j] >= 0) x = RowIO<RT>::unpack(raw[j]);
+                if (dst[j] >= 0) x = RowIO<RT>::unpack(in[j]);
                 unsigned char *p = a.c.pool + (dst[j] * HD + sub * 8) * ST::SIZE;
                 if constexpr (SCALED) {
                     unsigned big = 0;
@@ -201,7 +220,7 @@ __global__ void __launch_bounds__(KR_THREADS) k_kv_rows(const KrArgs a) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) x.v[e] *= scale[j];
                 }
-                RowIO<RT>::store(base[j] + src[j], x);
+                RowIO<RT>::store(base[j], x);
             }
         }
     }
