@@ -285,7 +285,8 @@ enum {
 };
 
 /* Rows of heads: element e of head h of row r is data_dev[r * row_stride + h * head_stride + e] (strides in elements,
- * so that q, k and v can be parts of one projection's output).  data_dev and both strides must be multiples of 16 bytes. */
+ * so that q, k and v can be parts of one projection's output).  data_dev and both strides must be multiples of 16 bytes.
+ * A stride of zero repeats a row or a head of an input (not in mdi_attn_prompt, whose tiles are copied by descriptor). */
 typedef struct {
     void *data_dev;
     int dtype;                       /* MDI_DTYPE_* */
@@ -324,11 +325,11 @@ int mdi_kv_read(const mdi_kv_cache *cache, int n_seq, const int32_t *slot_dev, c
 
 /* Attention of one new token per sequence over the cached rows 0 .. len_dev[i]-1 of its slot (its own row already appended):
  * out[i][h] = sum_j softmax_j(scale * q[i][h] . K_j) V_j with K, V of key/value head h / (n_head / n_kv_head).  q, out: n_seq
- * rows of n_head heads, of the same dtype.  len 0 gives zeros; an infinity among the values gives NaN in its
- * element of the output.  max_len: an upper bound of the lengths (0: what the page
+ * rows of n_head heads, of the same dtype.  A sequence of which nothing is left (length 0, all its pages
+ * missing) or whose scores are all -inf gives zeros; an infinity among the values gives NaN in its element of the output.  max_len: an upper bound of the lengths (0: what the page
  * table can hold); it only decides over how many blocks a sequence is split, longer sequences are still read whole.
  * workspace_dev: mdi_attn_decode_workspace() bytes (its contents do not matter), 16-byte aligned, used by one call at a
- * time.  scale > 0. */
+ * time.  0 < scale <= 1e38. */
 int64_t mdi_attn_decode_workspace(const mdi_kv_cache *cache, int n_seq, int n_head, int max_len);
 int mdi_attn_decode(const mdi_kv_cache *cache, int n_seq, const int32_t *slot_dev, const int32_t *len_dev, int max_len, int n_head,
                     const mdi_rows *q, const mdi_rows *out, float scale, void *workspace_dev, int64_t workspace_bytes,
@@ -337,9 +338,9 @@ int mdi_attn_decode(const mdi_kv_cache *cache, int n_seq, const int32_t *slot_de
 /* Causal attention over packed sequences (first visits: whole prompts, or the next chunk of a prompt behind rows that are cached
  * already).  Sequence i: query rows q_start_dev[i] .. q_start_dev[i+1]-1 of q, key/value rows k_start_dev[i] .. k_start_dev[i+1]-1 of
  * k and v.  Its last query row sees all its keys, the one before all but the last, and so on; a row that sees nothing
- * (more queries than keys) gives zeros.  n_q_rows, n_k_rows: rows that q / out and k / v hold; rows of out at or behind
+ * (more queries than keys), or whose scores are all -inf, gives zeros.  n_q_rows, n_k_rows: rows that q / out and k / v hold, at most 2^30 each; rows of out at or behind
  * q_start_dev[n_seq] are left as they are.  q, k, v, out: one dtype, F16 or BF16; head_dim 16, 32, 64 or 128; n_head a multiple of
- * n_kv_head.  The weights are rounded to that dtype before they meet the values, sums are fp32.  scale > 0. */
+ * n_kv_head.  The weights are rounded to that dtype before they meet the values, sums are fp32.  0 < scale <= 1e38. */
 int mdi_attn_prompt(int n_seq, const int32_t *q_start_dev, const int32_t *k_start_dev, int n_q_rows, int n_k_rows, int n_head, int n_kv_head,
                     int head_dim, const mdi_rows *q, const mdi_rows *k, const mdi_rows *v, const mdi_rows *out, float scale,
                     int32_t *status_dev, void *stream);

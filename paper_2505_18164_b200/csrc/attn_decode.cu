@@ -2,8 +2,7 @@
 //     out[i][h] = sum_j softmax_j(scale * q[i][h] . K_j) V_j,   j < len[i],   K, V of key/value head h / group.
 //
 // Bound: the bytes of the cached rows.  What the layout is for:
-//  * Work is cut into tiles of cached rows: 16 (16-bit types) or 32 (8-bit types: as many bytes; one softmax step serves
-//    twice the rows), in units of 16 that never cross a page.  All tiles of all (sequence, key/value head,
+//  * Work is cut into tiles of 32 cached rows, in units of 16 that never cross a page.  All tiles of all (sequence, key/value head,
 //    chunk of up to 8 of its query heads) are laid end to end and dealt to the warps of the launch in equal contiguous
 //    shares, so sequences of any mix of lengths keep every warp equally busy.  A (sequence, head) that a share boundary
 //    cuts leaves partial results (maximum, sum, unnormalised output) in the workspace; a second, small kernel joins them in
@@ -33,27 +32,15 @@
 namespace mdi {
 namespace {
 
-#ifndef AD_WARPS_DEF
-#define AD_WARPS_DEF 4
-#endif
-constexpr int AD_WARPS = AD_WARPS_DEF;      // warps per block (they share nothing but the table of lengths)
+constexpr int AD_WARPS = 4;      // warps per block (they share nothing but the table of lengths)
 constexpr int AD_THREADS = AD_WARPS * 32;
-#ifndef AD_U8
-#define AD_U8 2
-#define AD_U16 2
-#endif
-#ifndef AD_MAXB
-#define AD_MAXB 4
-#endif
-#ifndef AD_STAGES_DEF
-#define AD_STAGES_DEF 2
-#endif
+constexpr int AD_UNITS = 2;      // 16-row units per tile: one softmax step serves 32 rows.  16 rows: 86 instead of 78 us (int8, 32 x 128 heads, 16 x 2600 rows), 39 instead of 32 us (bf16, 40 heads on 8, 64 ragged sequences)
+constexpr int AD_STAGES = 2;     // tiles in a warp's ring.  3 leave room for fewer blocks: 4 to 9% slower
+constexpr int AD_MAX_BLOCKS = 4; // resident blocks per SM
 constexpr int AD_MAX_SEQ = 256;  // sequences per launch (their table shares shared memory with the rings of 4 blocks per SM)
 constexpr int AD_HC = 8;         // query heads per chunk
 constexpr int AD_SM = 148;
-#ifndef AD_TURN
-#define AD_TURN 2
-#endif
+constexpr int AD_TURN = 2;       // see ad_places (1, 2, 4: within 2%; 0: 44 instead of 32 us for the ragged sequences above)
 constexpr float AD_SLACK = 4.f;  // a maximum may be exceeded by 2^4 before what has been summed is rescaled
 constexpr int AD_JOIN_THREADS = 128;
 
@@ -72,7 +59,6 @@ enum { AD_I8, AD_E4M3, AD_F16, AD_BF16 };
 template <int ST> struct AdStore {
     static constexpr int SIZE = ST <= AD_E4M3 ? 1 : 2;
     static constexpr bool SCALED = SIZE == 1, BF = ST == AD_BF16;
-    static constexpr int U = SIZE == 1 ? AD_U8 : AD_U16;       // 16-row units per tile
 };
 
 __device__ __forceinline__ void ad_mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, std::false_type) {
@@ -163,12 +149,12 @@ template <int ST, int HD> struct AdTile {
     static constexpr int SZ = AdStore<ST>::SIZE, RB = HD * SZ;
     static constexpr int KB = RB / 4, KC = KB < 16 ? KB : 16, KN = KB / KC;
     static constexpr int VB = RB / 8, VC = VB < 16 ? VB : 16, VN = VB / VC;
-    static constexpr int U = AdStore<ST>::U, ROWS = 16 * U;
+    static constexpr int U = AD_UNITS, ROWS = 16 * U;
     static constexpr int K_BYTES = 16 * RB, UNIT = 2 * K_BYTES;
     static constexpr int SCALES = U * UNIT, LIVE = SCALES + (SZ == 1 ? U * 128 : 0); // per unit 16 + 16 scales, then the number of rows
-    static constexpr int STAGE = LIVE + 16, STAGES = AD_STAGES_DEF;
+    static constexpr int STAGE = LIVE + 16, STAGES = AD_STAGES;
     static constexpr int BLOCK_SMEM = AD_WARPS * STAGES * STAGE + (AD_MAX_SEQ + 1) * 8 + AD_MAX_SEQ * 4;
-    static constexpr int FIT = (227 * 1024) / (BLOCK_SMEM + 1024), BLOCKS = FIT < AD_MAXB ? FIT : AD_MAXB; // resident blocks per SM
+    static constexpr int FIT = (227 * 1024) / (BLOCK_SMEM + 1024), BLOCKS = FIT < AD_MAX_BLOCKS ? FIT : AD_MAX_BLOCKS; // resident blocks per SM
     static __device__ __forceinline__ int at(int row, int byte) {
         const int sw = RB >= 128 ? row & 7 : RB == 64 ? (row >> 1) & 3 : 0;
         return row * RB + ((byte & ~15) ^ (sw << 4)) + (byte & 15);
@@ -190,11 +176,13 @@ __device__ __forceinline__ int ad_len(const AdArgs &a, int i, int *status) {
 // finish a pair and begin the next: without them, shares full of very short sequences take far longer than the others.
 __device__ __forceinline__ int ad_places(int n_tiles) { return n_tiles > 0 ? n_tiles + AD_TURN : 0; }
 
+template <int ROWS> __device__ __forceinline__ int ad_tiles(int len) { return (int)(((unsigned)len + ROWS - 1) / ROWS); }
+
 // Where in the line: sequence, (head, chunk) pair within it, tile within the pair
 template <int ROWS> struct AdCursor {
     int i, pair, tile, n_tiles, len;
     long long at; // its place
-    __device__ __forceinline__ void enter(const int *s_len, int seq) { i = seq; len = s_len[seq]; n_tiles = (len + ROWS - 1) / ROWS; }
+    __device__ __forceinline__ void enter(const int *s_len, int seq) { i = seq; len = s_len[seq]; n_tiles = ad_tiles<ROWS>(len); }
     // the first tile at or behind place `first`
     __device__ __forceinline__ void seek(const long long *pref, const int *s_len, int n_seq, int pairs, long long first) {
         int lo = 0, hi = n_seq - 1; // last sequence that begins at or before it
@@ -203,9 +191,10 @@ template <int ROWS> struct AdCursor {
             if (pref[mid] * pairs <= first) lo = mid; else hi = mid - 1;
         }
         enter(s_len, lo);
-        const int in = (int)(first - pref[lo] * pairs), per = ad_places(n_tiles); // a sequence has fewer than 2^31 places
-        pair = in / per;
-        tile = in - pair * per;
+        const long long in = first - pref[lo] * pairs;
+        const int per = ad_places(n_tiles);
+        pair = in <= 0x7fffffff ? (int)in / per : (int)(in / per); // (a 32-bit division where it will do)
+        tile = (int)(in - (long long)pair * per);
         at = first;
         if (tile >= n_tiles) {
             at += per - tile;
@@ -259,7 +248,7 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
         for (int base = 0; base < a.n_seq; base += AD_THREADS) {
             const int i = base + tid;
             const int n = i < a.n_seq ? ad_len(a, i, blockIdx.x == 0 ? a.status : nullptr) : 0;
-            const long long mine = ad_places((n + TL::ROWS - 1) / TL::ROWS);
+            const long long mine = ad_places(ad_tiles<TL::ROWS>(n));
             long long incl = mine;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -309,8 +298,8 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
                 batch_tile = nxt.tile;
                 page_slot = a.c.slot ? a.c.slot[nxt.i] : a.seq0 + nxt.i;
                 batch_page = -1;
-                const int row = (batch_tile * U + lane) << 4;
-                if (row < nxt.len) {
+                const unsigned row = (unsigned)(batch_tile * U + lane) << 4; // (may pass 2^31 next to the largest length)
+                if (row < (unsigned)nxt.len) {
                     batch_page = __ldg(a.c.table + (long long)page_slot * a.c.table_stride + (row >> a.c.page_shift));
                     if ((unsigned)batch_page >= (unsigned)a.c.n_pages) { op_status(a.status, MDI_STATUS_PAGE); batch_page = -1; }
                 }
@@ -321,12 +310,12 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
             int page = -1;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int row0 = (nxt.tile * U + u) << 4;
+                const unsigned row0 = (unsigned)(nxt.tile * U + u) << 4;
                 if (u == 0 || a.c.page_shift == 4) {
                     page = __shfl_sync(0xffffffffu, batch_page, (nxt.tile - batch_tile) * U + u);
-                    kr = page < 0 ? 0 : ((((long long)page * 2) * a.c.n_kv_head + h) << a.c.page_shift) + (row0 & ((1 << a.c.page_shift) - 1));
+                    kr = page < 0 ? 0 : ((((long long)page * 2) * a.c.n_kv_head + h) << a.c.page_shift) + (int)(row0 & ((1u << a.c.page_shift) - 1));
                 } else kr += page < 0 ? 0 : 16;
-                const int rows = page < 0 ? 0 : min(16, nxt.len - row0);
+                const int rows = page < 0 ? 0 : min(16, (int)((unsigned)nxt.len - row0));
                 const unsigned char *kp = a.c.pool + kr * TL::RB + lane * 16, *vp = kp + head_rows * TL::RB;
                 const uint32_t sk = st + u * TL::UNIT;
                 constexpr int COPIES = TL::K_BYTES / 512; // of 32 chunks; rows of 16 bytes: half of one
@@ -466,12 +455,13 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
             }
         }
         // ---- what the weights refer to: the largest score, plus the exponent of the largest value scale (weight times scale is
-        // what has to fit fp16; numerator and denominator share the reference), rounded up; it moves only when exceeded by the slack
+        // what has to fit fp16; numerator and denominator share the reference); it moves only when exceeded by the slack.  The bounds on
+        // the exponent keep the weights' sum finite for 2^31 rows (weights up to 2^(80 + 14)) and the largest weight above 2^-114.
         float top = x[0], big = vs[0];
 #pragma unroll
         for (int i = 1; i < 4 * U; ++i) { top = fmaxf(top, x[i]); big = fmaxf(big, vs[i]); }
         top = top * q_up - UP;
-        if (SCALED) top += ad_log2(fminf(fmaxf(big, 0x1p-90f), 0x1p90f));
+        if (SCALED) top += ad_log2(fminf(fmaxf(big, 0x1p-80f), 0x1p119f));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
         const bool rise = top > m + AD_SLACK || (m == -INFINITY && top > -INFINITY);
@@ -545,7 +535,7 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 if (2 * t + b >= n_here) continue;
-                const float inv = 1.f / (b ? l1 : l0);
+                const float sum = b ? l1 : l0, inv = sum == 0.f ? 0.f : 1.f / sum; // 0: no row is left, or all scores are -inf
                 RT *out = (RT *)a.out.data + was.i * a.out.row_stride + (h * a.group + ch * AD_HC + 2 * t + b) * a.out.head_stride;
 #pragma unroll
                 for (int k = 0; k < KS; ++k) {
@@ -574,7 +564,7 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
 // Joins what the shares left of a (sequence, query head); NW warps per head, grid (heads / (4 / NW), n_seq).  Sequences without
 // rows get zeros.  What to join follows from the lengths alone, so that is worked out before waiting for the main kernel.
 template <typename RT, int HD, int NW>
-__global__ void __launch_bounds__(AD_JOIN_THREADS) k_attn_decode_join(const AdArgs a, int rows_per_tile) {
+__global__ void __launch_bounds__(AD_JOIN_THREADS) k_attn_decode_join(const AdArgs a) {
     constexpr int EPL = HD >= 32 ? HD / 32 : 1, AHEAD = 8;
     __shared__ float sm_m[4], sm_l[4], sm_o[4][HD];
     __shared__ long long sm_before[4], sm_total[4];
@@ -582,7 +572,7 @@ __global__ void __launch_bounds__(AD_JOIN_THREADS) k_attn_decode_join(const AdAr
     const int hq = blockIdx.x * (4 / NW) + warp / NW, part_no = warp % NW;
     long long before = 0, total = 0;
     for (int j = tid; j < a.n_seq; j += AD_JOIN_THREADS) {
-        const long long n = ad_places((ad_len(a, j, nullptr) + rows_per_tile - 1) / rows_per_tile);
+        const long long n = ad_places(ad_tiles<16 * AD_UNITS>(ad_len(a, j, nullptr)));
         total += n;
         if (j < i) before += n;
     }
@@ -595,7 +585,7 @@ __global__ void __launch_bounds__(AD_JOIN_THREADS) k_attn_decode_join(const AdAr
     __syncthreads();
     before = (sm_before[0] + sm_before[1]) + (sm_before[2] + sm_before[3]);
     total = (sm_total[0] + sm_total[1]) + (sm_total[2] + sm_total[3]);
-    const int n_tiles = (ad_len(a, i, nullptr) + rows_per_tile - 1) / rows_per_tile;
+    const int n_tiles = ad_tiles<16 * AD_UNITS>(ad_len(a, i, nullptr));
     const bool mine = hq < a.n_head;
     RT *out = (RT *)a.out.data + i * a.out.row_stride + (mine ? hq : 0) * a.out.head_stride;
     int w0 = 0, w1 = 0, hg = 0;
@@ -678,7 +668,7 @@ __global__ void __launch_bounds__(AD_JOIN_THREADS) k_attn_decode_join(const AdAr
                 if (HD >= 32 || lane < HD) o[e] = o[e] * f0 + sm_o[w][lane + 32 * e] * f1;
         }
     }
-    const float inv = 1.f / l;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
     for (int e = 0; e < EPL; ++e)
         if (HD >= 32 || lane < HD) out[lane + 32 * e] = (RT)(o[e] * inv);
@@ -705,7 +695,7 @@ AdPlan ad_plan(const mdi_kv_cache *c, int n_seq, int n_head, int max_len) {
     p.chunks = (group + AD_HC - 1) / AD_HC;
     p.hc = std::min(group, AD_HC);
     const int64_t cap = (int64_t)c->pages_per_seq * c->page_tokens, len = max_len > 0 ? std::min<int64_t>(max_len, cap) : cap;
-    const int rows = 16 * (op_scaled(c) ? AD_U8 : AD_U16);
+    const int rows = 16 * AD_UNITS;
     const int64_t tiles = (int64_t)std::min(n_seq, AD_MAX_SEQ) * c->n_kv_head * p.chunks * ((len + rows - 1) / rows);
     // a share of fewer tiles would leave more bytes of partial results than it reads
     p.min_tiles = 2 + p.hc / 2;
@@ -734,8 +724,7 @@ template <typename RT, int ST, int HD> cudaError_t ad_launch(const AdArgs &a, in
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    const int rows = AdTile<ST, HD>::ROWS;
-    return wide ? cudaLaunchKernelEx(&cfg, k_attn_decode_join<RT, HD, 4>, a, rows) : cudaLaunchKernelEx(&cfg, k_attn_decode_join<RT, HD, 1>, a, rows);
+    return wide ? cudaLaunchKernelEx(&cfg, k_attn_decode_join<RT, HD, 4>, a) : cudaLaunchKernelEx(&cfg, k_attn_decode_join<RT, HD, 1>, a);
 }
 template <typename RT, int ST> cudaError_t ad_hd(const AdArgs &a, int blocks, cudaStream_t st) {
     switch (a.c.head_dim) {
@@ -781,16 +770,16 @@ extern "C" int mdi_attn_decode(const mdi_kv_cache *cache, int n_seq, const int32
     int rc = ad_check(who, cache, n_seq, n_head, max_len);
     if (rc != MDI_OK) return rc;
     if (!slot_dev && n_seq > cache->n_slots) return op_fail(MDI_ERR_ARG, "%s: %d sequences, but the page table has %d slots", who, n_seq, cache->n_slots);
-    if (!(scale > 0.f) || scale > 3e38f) return op_fail(MDI_ERR_ARG, "%s: scale must be positive and finite", who);
-    if ((rc = op_check_rows(who, "q", q, n_seq, n_head)) != MDI_OK) return rc;
-    if ((rc = op_check_rows(who, "out", out, n_seq, n_head)) != MDI_OK) return rc;
+    if (!(scale > 0.f) || scale > 1e38f) return op_fail(MDI_ERR_ARG, "%s: scale must be positive and at most 1e38", who);
+    if ((rc = op_check_rows(who, "q", q, n_seq, n_head, false)) != MDI_OK) return rc;
+    if ((rc = op_check_rows(who, "out", out, n_seq, n_head, true)) != MDI_OK) return rc;
     if (q->dtype != out->dtype) return op_fail(MDI_ERR_ARG, "%s: q and out differ in dtype", who);
     const AdPlan p = ad_plan(cache, std::max(n_seq, 1), n_head, max_len);
     if (n_seq > 0 && (!workspace_dev || workspace_bytes < p.bytes || ((uintptr_t)workspace_dev & 15)))
         return op_fail(MDI_ERR_ARG, "%s: needs a 16-byte aligned workspace of %lld bytes", who, (long long)p.bytes);
     if ((rc = op_check_ptrs(who, {{"pool_dev", cache->pool_dev, false}, {"scale_dev", cache->scale_dev, !op_scaled(cache)}, {"page_table_dev", cache->page_table_dev, false},
                                   {"q", q->data_dev, n_seq == 0}, {"out", out->data_dev, n_seq == 0}, {"slot_dev", slot_dev, true},
-                                  {"len_dev", len_dev, false}, {"workspace_dev", workspace_dev, true}, {"status_dev", status_dev, true}})) != MDI_OK)
+                                  {"len_dev", len_dev, n_seq == 0}, {"workspace_dev", workspace_dev, true}, {"status_dev", status_dev, true}})) != MDI_OK)
         return rc;
     for (int i0 = 0; i0 < n_seq; i0 += AD_MAX_SEQ) {
         AdArgs a{};

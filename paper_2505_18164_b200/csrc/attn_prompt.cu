@@ -40,7 +40,7 @@ constexpr int AP_ROWS = 128;              // rows of a sub-tile, keys of a tile
 constexpr int AP_THREADS = 640;
 constexpr int AP_SM = 148;                // blocks: one per SM
 constexpr int AP_SORT = 64;               // up to this many sequences their tiles are taken in order of the keys they see
-constexpr unsigned long long AP_WAIT_NS = 2000000000ull;
+constexpr unsigned long long AP_WAIT_NS = 2000000000ull, AP_WAIT_KEY_NS = 100; // longest wait: this, and that per key (some warps wait for the end of an item; a key takes 10 to 20 ns)
 
 struct ApArgs {
     OpRows v, out;
@@ -49,6 +49,7 @@ struct ApArgs {
     int n_seq, n_q, n_k, n_head, group, hd;
     int q_swap, k_swap, v_swap; // the tensor map has (element, row, head) instead of (element, head, row)
     float scale_log2e;
+    unsigned long long wait_ns; // longest wait
 };
 
 template <int HDP> struct ApLayout {
@@ -82,7 +83,7 @@ __device__ __forceinline__ void ap_expect(uint32_t bar, uint32_t bytes) {
 }
 // false: the wait gave up, or another one of the block did.  SLEEP: the thread may sleep between its looks; waking up then takes some
 // 180 clocks longer, but a sleeping warp takes no issue slots from the softmax warps of the other sub-tile.
-template <bool SLEEP> __device__ __noinline__ bool ap_wait_slow(uint32_t bar, uint32_t parity, int *abort, int *status) {
+template <bool SLEEP> __device__ __noinline__ bool ap_wait_slow(uint32_t bar, uint32_t parity, int *abort, int *status, unsigned long long wait_ns) {
     const unsigned long long t0 = tg_now();
     for (unsigned it = 0;; ++it) {
         if (SLEEP) {
@@ -93,7 +94,7 @@ template <bool SLEEP> __device__ __noinline__ bool ap_wait_slow(uint32_t bar, ui
         } else if (tg_try_wait(bar, parity)) return true;
         if (SLEEP || (it & 15u) == 15u) {
             if (*(volatile int *)abort) return false;
-            if (tg_now() - t0 > AP_WAIT_NS) break;
+            if (tg_now() - t0 > wait_ns) break;
         }
     }
     *(volatile int *)abort = 1;
@@ -111,9 +112,9 @@ template <int HDP> __device__ __forceinline__ void ap_load(uint32_t dst, const C
 }
 // ---- issued by a whole warp in step (one elected lane): the compiler can then keep descriptors in uniform registers; with one
 // thread of a diverged warp issuing, moving them there took longer than the products (90 instead of 64 clocks each)
-template <bool SLEEP = true> __device__ __forceinline__ bool ap_wait_warp(uint32_t bar, uint32_t parity, int *abort, int *status) {
+template <bool SLEEP = true> __device__ __forceinline__ bool ap_wait_warp(uint32_t bar, uint32_t parity, int *abort, const ApArgs &a) {
     bool ok = tg_try_wait(bar, parity);
-    if (!__all_sync(0xffffffffu, ok)) ok = ok || ap_wait_slow<SLEEP>(bar, parity, abort, status);
+    if (!__all_sync(0xffffffffu, ok)) ok = ok || ap_wait_slow<SLEEP>(bar, parity, abort, a.status, a.wait_ns);
     return __all_sync(0xffffffffu, ok);
 }
 // named barriers of the softmax warps
@@ -311,7 +312,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
     // Every warp waits for an item, reads what it wants of it from shared memory and says when it has (the softmax warps at the item's
     // end: what is held in registers meanwhile would be spilled, and with all this shared memory there is next to no first-level cache
     // behind the spills).
-    auto arrived = [&](int it) { return ap_wait_warp(b_ifull + 8 * (it & 1), (it >> 1) & 1, abort, a.status); };
+    auto arrived = [&](int it) { return ap_wait_warp(b_ifull + 8 * (it & 1), (it >> 1) & 1, abort, a); };
     auto done_with = [&](int it) {
         __syncwarp();
         if (lane == 0) ap_arrive(b_iempty + 8 * (it & 1));
@@ -319,7 +320,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
 
     if (warp == 19) { // ---- items: the blocks take them in turn, to and fro, so that each gets long and short ones alike
         for (int it = 0;; ++it) {
-            if (it >= 2 && !ap_wait_warp(b_iempty + 8 * (it & 1), ((it >> 1) & 1) ^ 1, abort, a.status)) break;
+            if (it >= 2 && !ap_wait_warp(b_iempty + 8 * (it & 1), ((it >> 1) & 1) ^ 1, abort, a)) break;
             const long long x = (long long)it * gridDim.x + (it & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
             ApItem *i = &sh->item[it & 1];
             ap_find_tile(a, (int)min(x / a.n_head, (long long)0x7fffffff), lane, it == 0 && blockIdx.x == 0, i);
@@ -340,7 +341,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             bool ok = true;
             for (int i = 0; i < 2 * n_tiles && ok; ++i, ++n) {
                 const int st = n % NST;
-                if (n >= NST) ok = ap_wait_warp(b_empty + 8 * st, ((n / NST) & 1) ^ 1, abort, a.status);
+                if (n >= NST) ok = ap_wait_warp(b_empty + 8 * st, ((n / NST) & 1) ^ 1, abort, a);
                 if (!ok) break;
                 if (lane == 0) {
                     ap_expect(b_full + 8 * st, L::TILE);
@@ -350,7 +351,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                     else ap_load<HDP>(dst, &tm_k, a.k_swap, kvh, row, b_full + 8 * st);
                 }
                 if (i == 0) { // the queries, once the previous item's are no longer needed
-                    if (items > 0) ok = ap_wait_warp(b_qempty, (items - 1) & 1, abort, a.status);
+                    if (items > 0) ok = ap_wait_warp(b_qempty, (items - 1) & 1, abort, a);
                     if (ok && lane == 0) {
                         ap_expect(b_qfull, ((nt0 > 0) + (nt1 > 0)) * L::TILE);
                         if (nt0 > 0) ap_load<HDP>(s_base + L::Q, &tm_q, a.q_swap, head, q_row, b_qfull);
@@ -363,8 +364,8 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         }
         if (*(volatile int *)abort) { // nothing may land in this memory after the block has gone
             int mine = 0;
-            if (items > 0) ap_wait_warp(b_qfull, (items - 1) & 1, &mine, a.status);
-            for (int i = max(0, n - NST); i < n; ++i) ap_wait_warp(b_full + 8 * (i % NST), (i / NST) & 1, &mine, a.status);
+            if (items > 0) ap_wait_warp(b_qfull, (items - 1) & 1, &mine, a);
+            for (int i = max(0, n - NST); i < n; ++i) ap_wait_warp(b_full + 8 * (i % NST), (i / NST) & 1, &mine, a);
         }
     } else if (warp > 16) { // ---- MMA: the whole warp, see ap_mma_ss
         const uint32_t fmt = (1u << 4) | (BF ? (1u << 7) | (1u << 10) : 0u) | ((uint32_t)(AP_ROWS >> 4) << 24);
@@ -381,14 +382,14 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                 done_with(it);
                 if (last) break;
                 if (n_all == 0) continue;
-                ok = ap_wait_warp(b_qfull, items++ & 1, abort, a.status);
+                ok = ap_wait_warp(b_qfull, items++ & 1, abort, a);
                 for (int j = 0; j < n_all && ok; ++j) {
-                    ok = ap_wait_warp(b_full + 8 * st, par, abort, a.status);
+                    ok = ap_wait_warp(b_full + 8 * st, par, abort, a);
                     const uint32_t k = base + L::RING + st * L::TILE;
 #pragma unroll
                     for (int s = 0; s < 2; ++s) {
                         if (j >= (s ? nt1 : nt0) || !ok) continue;
-                        if (uses > 0) ok = ap_wait_warp<false>(b_free, (uses - 1) & 1, abort, a.status); // the previous scores have been taken
+                        if (uses > 0) ok = ap_wait_warp<false>(b_free, (uses - 1) & 1, abort, a); // the previous scores have been taken
                         if (!ok) continue;
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                         const uint32_t q = base + L::Q + s * L::TILE;
@@ -418,19 +419,19 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                 done_with(it);
                 if (last) break;
                 for (int j = 0; j < n_all && ok; ++j) {
-                    ok = ap_wait_warp(b_full + 8 * st, par, abort, a.status);
+                    ok = ap_wait_warp(b_full + 8 * st, par, abort, a);
                     const uint32_t v = base + L::RING + st * L::TILE;
 #pragma unroll
                     for (int s = 0; s < 2; ++s) {
                         if (j >= (s ? nt1 : nt0)) continue;
                         if (j == 0) { // the outputs of the sub-tile's previous item have been taken
-                            if (items[s] > 0) ok = ok && ap_wait_warp<false>(b_ofree + 8 * s, (items[s] - 1) & 1, abort, a.status);
+                            if (items[s] > 0) ok = ok && ap_wait_warp<false>(b_ofree + 8 * s, (items[s] - 1) & 1, abort, a);
                             ++items[s];
                         }
                         // weights of the keys 0-31 and 64-95, then of the others
 #pragma unroll
                         for (int step = 0; step < 2; ++step) {
-                            ok = ok && ap_wait_warp<false>(b_p + 16 * s + 8 * step, tiles[s] & 1, abort, a.status);
+                            ok = ok && ap_wait_warp<false>(b_p + 16 * s + 8 * step, tiles[s] & 1, abort, a);
                             if (!ok) break;
                             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
@@ -452,7 +453,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         if (!ok) { // no product may still run when the block goes
             int mine = 0;
             ap_commit(tg_smem_u32(&sh->drain[warp - 17]));
-            ap_wait_warp(tg_smem_u32(&sh->drain[warp - 17]), 0, &mine, a.status);
+            ap_wait_warp(tg_smem_u32(&sh->drain[warp - 17]), 0, &mine, a);
         }
     } else {
         // ---- softmax: sub-tile s, half of the keys of a tile; thread = row = tensor memory lane
@@ -462,187 +463,187 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         // Few registers are left beside a row's 64 scores: what can be read again from shared memory is.
         int t = 0, ring = 1;                     // tiles of this sub-tile so far; place in the ring (counted on) of the values of the tile `t`
         for (int it = 0;; ++it) {
-        bool ok = arrived(it);
-        const ApItem *item = &sh->item[it & 1];
-        if (ap_vote(9 + s, !ok, 256) || item->tile < 0) break; // all of the sub-tile's warps go on, or none
-        const int t_end = t + ap_key_tiles(item, s);
-        int here = min(item->nk - item->nq + (2 * item->tile + s) * AP_ROWS + r + 1, item->nk) - 64 * half; // keys of this half and on that the row sees
-        // first tile with a key that some row of the item does not see
-        const int t_masked = t + min(max(item->nk - item->nq + item->tile * 2 * AP_ROWS + 1, 0), item->nk) / AP_ROWS;
-        bool first = true;
-        float m = -INFINITY, l = 0.f; // what the weights refer to (in log2 units), sum of this thread's weights
-        for (; t < t_end; ++t, here -= AP_ROWS, ring += 2) {
-            // (after a wait that ran out a warp goes on to meet its partner at the barriers, and does nothing else)
-            ok = ok && ap_wait_warp(b_s + 8 * s, t & 1, abort, a.status);
-            if (!ok) {
-                if (ap_vote(two, false, 64)) { ap_meet(two, 64); ap_meet(two, 64); }
-                first = false;
-                continue;
-            }
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            uint32_t x[64];
-            ap_ld32(x, 0, t_s);
-            ap_ld32(x, 32, t_s + 32);
-            ap_wait_ld();
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) ap_arrive(b_free); // S may hold the other sub-tile's scores
-            if (__any_sync(0xffffffffu, here < 64)) {
-#pragma unroll
-                for (int e = 0; e < 64; ++e)
-                    if (e >= here) x[e] = 0xff800000u;
-            }
-            float t4[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) t4[u] = ap_max_nan(__uint_as_float(x[u]), __uint_as_float(x[4 + u]), __uint_as_float(x[8 + u]));
-#pragma unroll
-            for (int e = 12; e < 60; e += 8)
-#pragma unroll
-                for (int u = 0; u < 4; ++u) t4[u] = ap_max_nan(t4[u], __uint_as_float(x[e + u]), __uint_as_float(x[e + 4 + u]));
-#pragma unroll
-            for (int u = 0; u < 4; ++u) t4[u] = ap_max_nan(t4[u], __uint_as_float(x[60 + u]), t4[u]);
-            float top = ap_max_nan(ap_max_nan(t4[0], t4[1], t4[2]), t4[3], t4[3]);
-            if (!(top < INFINITY)) l = __uint_as_float(0x7fc00000u); // a score of +inf or NaN: the row is NaN
-            // does any row of the two warps need another reference?
-            const float c = a.scale_log2e;
-            const bool rise = m == -INFINITY ? top > -INFINITY : top * c - m > 8.f;
-            if (ap_vote(two, rise, 64)) {
-                sh->row[s][half][r] = top;
-                ap_meet(two, 64);
-                const float other = sh->row[s][half ^ 1][r], high = fmaxf(top, other); // (a NaN is dropped: its row's sum is NaN already)
-                const bool up = m == -INFINITY ? high > -INFINITY : high * c - m > 8.f;
-                const float f = up ? (m == -INFINITY ? 0.f : ap_exp2(m - high * c)) : 1.f;
-                if (up) m = high * c;
-                l *= f;
-                if (!first) { // half of O's columns each, once the product of the previous tile is in
-                    ok = ap_wait_warp(b_pv + 8 * s, (t - 1) & 1, abort, a.status);
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-#pragma unroll 1
-                    for (int o = half * (HDP / 2); o < (half + 1) * (HDP / 2); o += 16) { // (16 at a time: the 64 scores are held meanwhile)
-                        uint32_t y[16];
-                        ap_ld16(y, t_o + o);
-                        ap_wait_ld();
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(__uint_as_float(y[e]) * f);
-                        ap_st16(t_o + o, y, 0);
-                    }
-                    ap_wait_st();
-                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            bool ok = arrived(it);
+            const ApItem *item = &sh->item[it & 1];
+            if (ap_vote(9 + s, !ok, 256) || item->tile < 0) break; // all of the sub-tile's warps go on, or none
+            const int t_end = t + ap_key_tiles(item, s);
+            int here = min(item->nk - item->nq + (2 * item->tile + s) * AP_ROWS + r + 1, item->nk) - 64 * half; // keys of this half and on that the row sees
+            // first tile with a key that some row of the item does not see
+            const int t_masked = t + min(max(item->nk - item->nq + item->tile * 2 * AP_ROWS + 1, 0), item->nk) / AP_ROWS;
+            bool first = true;
+            float m = -INFINITY, l = 0.f; // what the weights refer to (in log2 units), sum of this thread's weights
+            for (; t < t_end; ++t, here -= AP_ROWS, ring += 2) {
+                // (after a wait that ran out a warp goes on to meet its partner at the barriers, and does nothing else)
+                ok = ok && ap_wait_warp(b_s + 8 * s, t & 1, abort, a);
+                if (!ok) {
+                    if (ap_vote(two, false, 64)) { ap_meet(two, 64); ap_meet(two, 64); }
+                    first = false;
+                    continue;
                 }
-                ap_meet(two, 64); // O is rescaled, and row[] may be written again
-            }
-            first = false;
-            if (t >= t_masked) { // values of this tile that may meet a weight of zero: infinities and NaN out (the 64 rows of this half)
-                ok = ok && ap_wait_warp(b_full + 8 * (ring % NST), (ring / NST) & 1, abort, a.status);
-                if (!ok) continue;
-                unsigned char *v = smem + L::RING + (ring % NST) * L::TILE + (64 * half + (r >> 1)) * 128; // two threads a row
-                constexpr int PART = HDP / 16; // 16-byte chunks each
-                const int c0 = (r & 1) * PART;
-                uint32_t bad = 0;
-#pragma unroll
-                for (int q = 0; q < PART; ++q) {
-                    const int ch = c0 + ((q + lane) & (PART - 1));
-                    const uint4 w = *(const uint4 *)(v + (ch >> 3) * (AP_ROWS * 128) + (ch & 7) * 16);
-                    bad |= ap_nonfinite<T>(w.x) | ap_nonfinite<T>(w.y) | ap_nonfinite<T>(w.z) | ap_nonfinite<T>(w.w);
-                }
-                if (bad) {
-                    *(volatile int *)&sh->poison[it & 3] = it + 1;
-                    __threadfence_block();
-                    for (int q = c0 * 4; q < (c0 + PART) * 4; ++q) {
-                        uint32_t *w = (uint32_t *)(v + (q >> 5) * (AP_ROWS * 128)) + (q & 31);
-                        const uint32_t f = ap_nonfinite<T>(*w);
-                        if (f) *w &= ~((f >> 15) * 0xffffu);
-                    }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                }
-            }
-            // The previous weights have been used.  (Waiting here rather than before the first store, half an exponential phase later,
-            // keeps the sub-tiles out of step: 2990 instead of 3400 clocks a tile.)
-            ok = ok && (t == 0 || ap_wait_warp(b_pv + 8 * s, (t - 1) & 1, abort, a.status));
-            if (!ok) continue;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const float ref = m == -INFINITY ? 0.f : m;
-            const ap_f2 c2 = ap_pair(c, c), r2 = ap_pair(-ref, -ref);
-            ap_f2 sum0 = ap_pair(0.f, 0.f), sum1 = sum0;
-            // (Replacing a quarter of the exponentials by polynomials on the multiply-add pipe made a tile 20% slower: the exponential
-            // unit is 70% busy, and the softmax warps' instructions, not it, are what the four warps of a scheduler queue for.)
-#pragma unroll
-            for (int step = 0; step < 2; ++step) {
-#pragma unroll
-                for (int e = 32 * step; e < 32 * step + 32; e += 2) {
-                    const ap_f2 y = ap_fma2(ap_pair(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), c2, r2);
-                    float p0, p1;
-                    ap_unpair(y, p0, p1);
-                    p0 = ap_exp2(p0);
-                    p1 = ap_exp2(p1);
-                    if (e % 4) sum1 = ap_add2(sum1, ap_pair(p0, p1)); else sum0 = ap_add2(sum0, ap_pair(p0, p1));
-                    x[e / 2] = ap_pack<T>(p0, p1);
-                }
-                ap_st16(t_p + 16 * step, x, 16 * step);
-                ap_wait_st();
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                uint32_t x[64];
+                ap_ld32(x, 0, t_s);
+                ap_ld32(x, 32, t_s + 32);
+                ap_wait_ld();
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) ap_arrive(b_p + 16 * s + 8 * step);
-            }
-            {
-                float s0, s1;
-                ap_unpair(ap_add2(sum0, sum1), s0, s1);
-                l += s0 + s1;
-            }
-        }
-        const int n_mine = ap_key_tiles(item, s);
-        ring += 2 * (max(ap_key_tiles(item, 0), ap_key_tiles(item, 1)) - n_mine); // the other sub-tile's
-        // ---- output: half of the columns each
-        const int seen = min(item->nk - item->nq + (2 * item->tile + s) * AP_ROWS + r + 1, item->nk);
-        const int row = (2 * item->tile + s) * AP_ROWS + r, nq = item->nq; // row of the sequence
-        const bool valid = row < nq;
-        T *out = (T *)a.out.data + (long long)(item->q0 + row) * a.out.row_stride + (long long)item->head * a.out.head_stride;
-        if (n_mine == 0) {
-            if (valid && half == 0)
-                for (int e = 0; e < a.hd; e += 8) *(uint4 *)(out + e) = make_uint4(0, 0, 0, 0);
-        } else {
-            sh->row[s][half][r] = l;
-            ap_meet(9 + s, 256); // the sums; and all of this sub-tile's looks at the values are done
-            ok = ok && ap_wait_warp(b_pv + 8 * s, (t - 1) & 1, abort, a.status);
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            // 32 columns at a time through shared memory, so that stores cover whole sectors side by side: a row per thread, 16 bytes at a
-            // time, took 2000 clocks more
-            unsigned char *mine = smem + L::OUT + warp * 2048;
-            const bool poison = *(volatile int *)&sh->poison[it & 3] == it + 1;
-            const float inv = seen > 0 ? 1.f / (sh->row[s][0][r] + sh->row[s][1][r]) : 0.f;
-#pragma unroll 1
-            for (int o = half * (HDP / 2); o < (half + 1) * (HDP / 2) && ok; o += 32) {
-                uint32_t y[32];
-                ap_ld32(y, 0, t_o + o);
-                ap_wait_ld();
+                if (lane == 0) ap_arrive(b_free); // S may hold the other sub-tile's scores
+                if (__any_sync(0xffffffffu, here < 64)) {
 #pragma unroll
-                for (int e = 0; e < 32; ++e) y[e] = seen > 0 ? __float_as_uint(__uint_as_float(y[e]) * inv) : 0u;
-#pragma unroll
-                for (int e = 0; e < 32; e += 8) {
-                    uint4 w;
-                    w.x = ap_pack<T>(__uint_as_float(y[e]), __uint_as_float(y[e + 1]));
-                    w.y = ap_pack<T>(__uint_as_float(y[e + 2]), __uint_as_float(y[e + 3]));
-                    w.z = ap_pack<T>(__uint_as_float(y[e + 4]), __uint_as_float(y[e + 5]));
-                    w.w = ap_pack<T>(__uint_as_float(y[e + 6]), __uint_as_float(y[e + 7]));
-                    *(uint4 *)(mine + lane * 64 + ((e / 8 ^ (lane >> 1 & 3)) * 16)) = w;
+                    for (int e = 0; e < 64; ++e)
+                        if (e >= here) x[e] = 0xff800000u;
                 }
-                if (poison && valid) ap_add_nonfinite<T>(a, mine + lane * 64, lane >> 1 & 3, item->kvh, item->k0 + min(max(item->nk - item->nq + item->tile * 2 * AP_ROWS + 1, 0), item->nk) / AP_ROWS * AP_ROWS, item->k0 + seen, o);
-                if (o + 32 == (half + 1) * (HDP / 2)) { // the last of this warp's columns: the next item's outputs may come
+                float t4[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) t4[u] = ap_max_nan(__uint_as_float(x[u]), __uint_as_float(x[4 + u]), __uint_as_float(x[8 + u]));
+#pragma unroll
+                for (int e = 12; e < 60; e += 8)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) t4[u] = ap_max_nan(t4[u], __uint_as_float(x[e + u]), __uint_as_float(x[e + 4 + u]));
+#pragma unroll
+                for (int u = 0; u < 4; ++u) t4[u] = ap_max_nan(t4[u], __uint_as_float(x[60 + u]), t4[u]);
+                float top = ap_max_nan(ap_max_nan(t4[0], t4[1], t4[2]), t4[3], t4[3]);
+                if (!(top < INFINITY)) l = __uint_as_float(0x7fc00000u); // a score of +inf or NaN: the row is NaN
+                // does any row of the two warps need another reference?
+                const float c = a.scale_log2e;
+                const bool rise = m == -INFINITY ? top > -INFINITY : top * c - m > 8.f;
+                if (ap_vote(two, rise, 64)) {
+                    sh->row[s][half][r] = top;
+                    ap_meet(two, 64);
+                    const float other = sh->row[s][half ^ 1][r], high = fmaxf(top, other); // (a NaN is dropped: its row's sum is NaN already)
+                    const bool up = m == -INFINITY ? high > -INFINITY : high * c - m > 8.f;
+                    const float f = up ? (m == -INFINITY ? 0.f : ap_exp2(m - high * c)) : 1.f;
+                    if (up) m = high * c;
+                    l *= f;
+                    if (!first) { // half of O's columns each, once the product of the previous tile is in
+                        ok = ap_wait_warp(b_pv + 8 * s, (t - 1) & 1, abort, a);
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll 1
+                        for (int o = half * (HDP / 2); o < (half + 1) * (HDP / 2); o += 16) { // (16 at a time: the 64 scores are held meanwhile)
+                            uint32_t y[16];
+                            ap_ld16(y, t_o + o);
+                            ap_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(__uint_as_float(y[e]) * f);
+                            ap_st16(t_o + o, y, 0);
+                        }
+                        ap_wait_st();
+                        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    }
+                    ap_meet(two, 64); // O is rescaled, and row[] may be written again
+                }
+                first = false;
+                if (t >= t_masked) { // values of this tile that may meet a weight of zero: infinities and NaN out (the 64 rows of this half)
+                    ok = ok && ap_wait_warp(b_full + 8 * (ring % NST), (ring / NST) & 1, abort, a);
+                    if (!ok) continue;
+                    unsigned char *v = smem + L::RING + (ring % NST) * L::TILE + (64 * half + (r >> 1)) * 128; // two threads a row
+                    constexpr int PART = HDP / 16; // 16-byte chunks each
+                    const int c0 = (r & 1) * PART;
+                    uint32_t bad = 0;
+#pragma unroll
+                    for (int q = 0; q < PART; ++q) {
+                        const int ch = c0 + ((q + lane) & (PART - 1));
+                        const uint4 w = *(const uint4 *)(v + (ch >> 3) * (AP_ROWS * 128) + (ch & 7) * 16);
+                        bad |= ap_nonfinite<T>(w.x) | ap_nonfinite<T>(w.y) | ap_nonfinite<T>(w.z) | ap_nonfinite<T>(w.w);
+                    }
+                    if (bad) {
+                        *(volatile int *)&sh->poison[it & 3] = it + 1;
+                        __threadfence_block();
+                        for (int q = c0 * 4; q < (c0 + PART) * 4; ++q) {
+                            uint32_t *w = (uint32_t *)(v + (q >> 5) * (AP_ROWS * 128)) + (q & 31);
+                            const uint32_t f = ap_nonfinite<T>(*w);
+                            if (f) *w &= ~((f >> 15) * 0xffffu);
+                        }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    }
+                }
+                // The previous weights have been used.  (Waiting here rather than before the first store, half an exponential phase later,
+                // keeps the sub-tiles out of step: 2990 instead of 3400 clocks a tile.)
+                ok = ok && (t == 0 || ap_wait_warp(b_pv + 8 * s, (t - 1) & 1, abort, a));
+                if (!ok) continue;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const float ref = m == -INFINITY ? 0.f : m;
+                const ap_f2 c2 = ap_pair(c, c), r2 = ap_pair(-ref, -ref);
+                ap_f2 sum0 = ap_pair(0.f, 0.f), sum1 = sum0;
+                // (Replacing a quarter of the exponentials by polynomials on the multiply-add pipe made a tile 20% slower: the exponential
+                // unit is 70% busy, and the softmax warps' instructions, not it, are what the four warps of a scheduler queue for.)
+#pragma unroll
+                for (int step = 0; step < 2; ++step) {
+#pragma unroll
+                    for (int e = 32 * step; e < 32 * step + 32; e += 2) {
+                        const ap_f2 y = ap_fma2(ap_pair(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), c2, r2);
+                        float p0, p1;
+                        ap_unpair(y, p0, p1);
+                        p0 = ap_exp2(p0);
+                        p1 = ap_exp2(p1);
+                        if (e % 4) sum1 = ap_add2(sum1, ap_pair(p0, p1)); else sum0 = ap_add2(sum0, ap_pair(p0, p1));
+                        x[e / 2] = ap_pack<T>(p0, p1);
+                    }
+                    ap_st16(t_p + 16 * step, x, 16 * step);
+                    ap_wait_st();
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                     __syncwarp();
-                    if (lane == 0) ap_arrive(b_ofree + 8 * s);
+                    if (lane == 0) ap_arrive(b_p + 16 * s + 8 * step);
                 }
-                __syncwarp();
-#pragma unroll
-                for (int i = 0; i < 4; ++i) { // 32 rows of 4 chunks, four neighbouring lanes on a row
-                    const int rr = i * 8 + lane / 4, ch = lane & 3, col = o + ch * 8, to = row - lane + rr;
-                    if (to < nq && col < a.hd)
-                        *(uint4 *)(out + (long long)(rr - lane) * a.out.row_stride + col) = *(const uint4 *)(mine + rr * 64 + ((ch ^ (rr >> 1 & 3)) * 16));
+                {
+                    float s0, s1;
+                    ap_unpair(ap_add2(sum0, sum1), s0, s1);
+                    l += s0 + s1;
                 }
-                __syncwarp();
             }
-        }
-        done_with(it);
+            const int n_mine = ap_key_tiles(item, s);
+            ring += 2 * (max(ap_key_tiles(item, 0), ap_key_tiles(item, 1)) - n_mine); // the other sub-tile's
+            // ---- output: half of the columns each
+            const int seen = min(item->nk - item->nq + (2 * item->tile + s) * AP_ROWS + r + 1, item->nk);
+            const int row = (2 * item->tile + s) * AP_ROWS + r, nq = item->nq; // row of the sequence
+            const bool valid = row < nq;
+            T *out = (T *)a.out.data + (long long)(item->q0 + row) * a.out.row_stride + (long long)item->head * a.out.head_stride;
+            if (n_mine == 0) {
+                if (valid && half == 0)
+                    for (int e = 0; e < a.hd; e += 8) *(uint4 *)(out + e) = make_uint4(0, 0, 0, 0);
+            } else {
+                sh->row[s][half][r] = l;
+                ap_meet(9 + s, 256); // the sums; and all of this sub-tile's looks at the values are done
+                ok = ok && ap_wait_warp(b_pv + 8 * s, (t - 1) & 1, abort, a);
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                // 32 columns at a time through shared memory, so that stores cover whole sectors side by side: a row per thread, 16 bytes at a
+                // time, took 2000 clocks more
+                unsigned char *mine = smem + L::OUT + warp * 2048;
+                const bool poison = *(volatile int *)&sh->poison[it & 3] == it + 1;
+                const float sum = sh->row[s][0][r] + sh->row[s][1][r], inv = seen > 0 && sum != 0.f ? 1.f / sum : 0.f; // (0: all scores are -inf)
+#pragma unroll 1
+                for (int o = half * (HDP / 2); o < (half + 1) * (HDP / 2) && ok; o += 32) {
+                    uint32_t y[32];
+                    ap_ld32(y, 0, t_o + o);
+                    ap_wait_ld();
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) y[e] = seen > 0 ? __float_as_uint(__uint_as_float(y[e]) * inv) : 0u;
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8) {
+                        uint4 w;
+                        w.x = ap_pack<T>(__uint_as_float(y[e]), __uint_as_float(y[e + 1]));
+                        w.y = ap_pack<T>(__uint_as_float(y[e + 2]), __uint_as_float(y[e + 3]));
+                        w.z = ap_pack<T>(__uint_as_float(y[e + 4]), __uint_as_float(y[e + 5]));
+                        w.w = ap_pack<T>(__uint_as_float(y[e + 6]), __uint_as_float(y[e + 7]));
+                        *(uint4 *)(mine + lane * 64 + ((e / 8 ^ (lane >> 1 & 3)) * 16)) = w;
+                    }
+                    if (poison && valid) ap_add_nonfinite<T>(a, mine + lane * 64, lane >> 1 & 3, item->kvh, item->k0 + min(max(item->nk - item->nq + item->tile * 2 * AP_ROWS + 1, 0), item->nk) / AP_ROWS * AP_ROWS, item->k0 + seen, o);
+                    if (o + 32 == (half + 1) * (HDP / 2)) { // the last of this warp's columns: the next item's outputs may come
+                        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) ap_arrive(b_ofree + 8 * s);
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) { // 32 rows of 4 chunks, four neighbouring lanes on a row
+                        const int rr = i * 8 + lane / 4, ch = lane & 3, col = o + ch * 8, to = row - lane + rr;
+                        if (to < nq && col < a.hd)
+                            *(uint4 *)(out + (long long)(rr - lane) * a.out.row_stride + col) = *(const uint4 *)(mine + rr * 64 + ((ch ^ (rr >> 1 & 3)) * 16));
+                    }
+                    __syncwarp();
+                }
+            }
+            done_with(it);
         }
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -692,15 +693,16 @@ extern "C" int mdi_attn_prompt(int n_seq, const int32_t *q_start_dev, const int3
     if (n_seq < 0 || n_q_rows < 0 || n_k_rows < 0) return op_fail(MDI_ERR_ARG, "%s: negative n_seq, n_q_rows or n_k_rows", who);
     if (head_dim != 16 && head_dim != 32 && head_dim != 64 && head_dim != 128) return op_fail(MDI_ERR_SHAPE, "%s: head_dim must be 16, 32, 64 or 128", who);
     if (n_kv_head < 1 || n_head < 1 || n_head % n_kv_head || n_head > 65535) return op_fail(MDI_ERR_SHAPE, "%s: n_head must be a multiple of n_kv_head", who);
-    if (!(scale > 0.f) || scale > 3e38f) return op_fail(MDI_ERR_ARG, "%s: scale must be positive and finite", who);
-    if ((rc = op_check_rows(who, "q", q, n_q_rows, n_head)) != MDI_OK) return rc;
-    if ((rc = op_check_rows(who, "k", k, n_k_rows, n_kv_head)) != MDI_OK) return rc;
-    if ((rc = op_check_rows(who, "v", v, n_k_rows, n_kv_head)) != MDI_OK) return rc;
-    if ((rc = op_check_rows(who, "out", out, n_q_rows, n_head)) != MDI_OK) return rc;
+    if (!(scale > 0.f) || scale > 1e38f) return op_fail(MDI_ERR_ARG, "%s: scale must be positive and at most 1e38", who);
+    if (n_q_rows > 1 << 30 || n_k_rows > 1 << 30) return op_fail(MDI_ERR_SHAPE, "%s: more than 2^30 rows", who);
+    if ((rc = op_check_rows(who, "q", q, n_q_rows, n_head, false)) != MDI_OK) return rc;
+    if ((rc = op_check_rows(who, "k", k, n_k_rows, n_kv_head, false)) != MDI_OK) return rc;
+    if ((rc = op_check_rows(who, "v", v, n_k_rows, n_kv_head, false)) != MDI_OK) return rc;
+    if ((rc = op_check_rows(who, "out", out, n_q_rows, n_head, true)) != MDI_OK) return rc;
     if ((q->dtype != MDI_DTYPE_F16 && q->dtype != MDI_DTYPE_BF16) || k->dtype != q->dtype || v->dtype != q->dtype || out->dtype != q->dtype)
         return op_fail(MDI_ERR_ARG, "%s: q, k, v and out must share one dtype, F16 or BF16", who);
     if ((rc = op_check_ptrs(who, {{"q", q->data_dev, n_q_rows == 0}, {"k", k->data_dev, n_k_rows == 0}, {"v", v->data_dev, n_k_rows == 0}, {"out", out->data_dev, n_q_rows == 0},
-                                  {"q_start_dev", q_start_dev, false}, {"k_start_dev", k_start_dev, false}, {"status_dev", status_dev, true}})) != MDI_OK)
+                                  {"q_start_dev", q_start_dev, n_seq == 0}, {"k_start_dev", k_start_dev, n_seq == 0}, {"status_dev", status_dev, true}})) != MDI_OK)
         return rc;
     for (const mdi_rows *r : {q, k, v})
         if ((r->row_stride == 0 && (r == q ? n_q_rows : n_k_rows) > 1) || (r->head_stride == 0 && (r == q ? n_head : n_kv_head) > 1))
@@ -719,6 +721,7 @@ extern "C" int mdi_attn_prompt(int n_seq, const int32_t *q_start_dev, const int3
     a.q_start = q_start_dev; a.k_start = k_start_dev; a.status = status_dev;
     a.n_seq = n_seq; a.n_q = n_q_rows; a.n_k = n_k_rows; a.n_head = n_head; a.group = n_head / n_kv_head; a.hd = head_dim;
     a.scale_log2e = scale * 1.4426950408889634f;
+    a.wait_ns = AP_WAIT_NS + AP_WAIT_KEY_NS * (unsigned long long)n_k_rows;
     const int64_t items = ((int64_t)n_q_rows / (2 * AP_ROWS) + std::min(n_seq, n_q_rows)) * n_head; // at most
     const dim3 grid((unsigned)std::min<int64_t>(items, AP_SM));
     cudaStream_t st = (cudaStream_t)stream;

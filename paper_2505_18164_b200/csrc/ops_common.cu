@@ -41,12 +41,13 @@ int op_check_ptrs(const char *who, std::initializer_list<OpPtr> ptrs) {
     return MDI_OK;
 }
 
-int op_check_rows(const char *who, const char *name, const mdi_rows *r, int rows, int heads) {
+int op_check_rows(const char *who, const char *name, const mdi_rows *r, int rows, int heads, bool written) {
     if (!r) return op_fail(MDI_ERR_ARG, "%s: %s is null", who, name);
     if (r->dtype != MDI_DTYPE_F32 && r->dtype != MDI_DTYPE_BF16 && r->dtype != MDI_DTYPE_F16) return op_fail(MDI_ERR_ARG, "%s: %s: unknown dtype", who, name);
     const int64_t unit = r->dtype == MDI_DTYPE_F32 ? 4 : 8; // elements in 16 bytes
     if (((uintptr_t)r->data_dev & 15) || (rows > 1 && r->row_stride % unit) || (heads > 1 && r->head_stride % unit))
         return op_fail(MDI_ERR_SHAPE, "%s: %s: the data and its strides must be multiples of 16 bytes", who, name);
+    if (written && ((rows > 1 && r->row_stride == 0) || (heads > 1 && r->head_stride == 0))) return op_fail(MDI_ERR_SHAPE, "%s: %s: a stride of an output is zero", who, name);
     if ((rows > 1 && r->row_stride < 0) || (heads > 1 && r->head_stride < 0)) return op_fail(MDI_ERR_SHAPE, "%s: %s: negative stride", who, name);
     return MDI_OK;
 }

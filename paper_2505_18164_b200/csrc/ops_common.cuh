@@ -20,8 +20,8 @@ int op_cuda(const char *who, cudaError_t e); // MDI_OK for cudaSuccess
 struct OpPtr { const char *name; const void *p; bool optional; };
 // every pointer must be device memory of the current device (null passes only where `optional`); checked last
 int op_check_ptrs(const char *who, std::initializer_list<OpPtr> ptrs);
-// a row view of `rows` rows of `heads` heads: type, alignment, strides (those of a dimension of size 1 do not matter)
-int op_check_rows(const char *who, const char *name, const mdi_rows *r, int rows, int heads);
+// a row view of `rows` rows of `heads` heads: type, alignment, strides (those of a dimension of size 1 do not matter; a zero one repeats an input, and is refused where `written`)
+int op_check_rows(const char *who, const char *name, const mdi_rows *r, int rows, int heads, bool written);
 int op_check_cache(const char *who, const mdi_kv_cache *c);
 inline bool op_scaled(const mdi_kv_cache *c) { return c->dtype == MDI_KV_I8 || c->dtype == MDI_KV_E4M3; }
 

@@ -4,8 +4,10 @@ Tolerances of the attention tests (worst cases, per output element, derived from
   scores      each of hd products and sums in fp32, the query possibly held as two 16-bit planes (2^-16 relative), the exponent's
               argument and the exponential to a few ulp:  ds = scale * sum_e |q_e k_e| * (2^-16 + hd 2^-23) + |score| 2^-21 + 2^-20
   weights     a relative error of a weight is at most 2 ds (its own and the denominator's), weights meet the values as two 16-bit
-              planes (decode: 2^-16) or rounded to the type (prompt: half a step, eps / 2, as the largest exact weight may lie
-              anywhere in its binade), and n additions in fp32 lose n 2^-23 of the sum of absolute values
+              planes (decode: 2^-16; one fp16, half a step of 2^-11, where the output is 16 bits and the cache is not bf16: with a
+              single row the weight times the value's scale is rounded once and the output once more, 2^-11 + 2^-8 together) or
+              rounded to the type (prompt: half a step, eps / 2, as the largest exact weight may lie anywhere in its binade), and n
+              additions in fp32 lose n 2^-23 of the sum of absolute values
   output      half a step of its type
 so |out - exact| <= (2 ds + w + n 2^-23) * sum_j p_j |v_j| + eps(out) / 2 * |exact| + the type's smallest step."""
 import math
@@ -274,7 +276,7 @@ def check_decode(c, q, out, lens, slots, dtype):
             assert (out[i] == 0).all()
             continue
         want, mag, ds = attend(q[i][:, None], c.get(0, slots[i], 0, ln), c.get(1, slots[i], 0, ln), c.hd ** -0.5, ints([ln]))
-        close(out[i][:, None], want, mag, ds, ln, 2.0 ** -15, dtype)
+        close(out[i][:, None], want, mag, ds, ln, 2.0 ** -15 + (2.0 ** -11 if dtype != F32 and c.store != BF16 else 0.0), dtype)
 
 
 @pytest.mark.parametrize("store", STORES)
@@ -364,6 +366,102 @@ def test_decode_lengths_out_of_range():
     mdi.attn_decode(c.handle, q, o, ints([48, 48, 48]), workspace=ws, slots=ints([0, 77, -1]), status=status)
     assert status.item() == mdi.STATUS_RANGE
     check_decode(c, q, o, [48, 0, 0], [0, 1, 2], F32)
+
+
+@pytest.mark.parametrize("store", [I8, BF16])
+@pytest.mark.parametrize("slots", [None, "other", "same"])
+def test_decode_of_more_sequences_than_a_launch_takes(store, slots):
+    n, heads, kv, hd, page = 600, 4, 2, 32, 16
+    c = Cache(store, kv, hd, page, 96, n, seed=21)
+    lens = [(37 * i) % 90 if i % 5 else 0 for i in range(n)]
+    lens[255], lens[256], lens[511], lens[512], lens[599] = 90, 1, 0, 77, 33
+    at = {None: list(range(n)), "other": [(7 * i + 3) % n for i in range(n)], "same": [5] * n}[slots]
+    for slot in sorted(set(at)):
+        k, v = (torch.randn(90, kv, hd, generator=gen(slot + j), device=DEV) for j in (0, 1000))
+        c.put(slot, 0, k, v)
+    q = torch.randn(n, heads, hd, generator=gen(1), device=DEV).to(BF16)
+    ws = torch.empty(max(1, mdi.attn_decode_workspace(c.handle, heads, 90, n_seq=n)), dtype=torch.uint8, device=DEV)
+    out, status = torch.full_like(q, 9.0), ints([0])
+    mdi.attn_decode(c.handle, q, out, ints(lens), 90, workspace=ws, slots=None if slots is None else ints(at), status=status)
+    assert status.item() == 0
+    check_decode(c, q, out, lens, at, BF16)
+
+
+@pytest.mark.parametrize("store", STORES)
+def test_decode_of_nothing(store):
+    """Zeros where no row is left: all pages missing, or all scores -inf; other sequences as before."""
+    lens = [40, 700, 33, 0]
+    c, q, out, ws, _ = decode_case(store, F32, 4, 2, 64, 16, lens, seed=22)
+    table, status = c.table.clone(), ints([0])
+    table[:2] = -1
+    h = mdi.KvCache(c.pool, table, scale=c.scale)
+    o = torch.full_like(q, 3.0)
+    mdi.attn_decode(h, q, o, ints(lens), workspace=ws, status=status)
+    assert status.item() == mdi.STATUS_PAGE
+    assert (o[0] == 0).all() and (o[1] == 0).all() and (o[3] == 0).all()
+    assert torch.equal(o[2], out[2])
+    if c.scale is None:
+        q[:, :, 0] = 1.0
+        for i in (0, 1):
+            for t in range(lens[i]):
+                c.pool[c.table[i, t // 16].item(), 0, 0, t % 16, 0] = -math.inf   # the first key head of both
+        mdi.attn_decode(c.handle, q, o, ints(lens), workspace=ws)
+        assert (o[:2, :2] == 0).all()
+        for i in (0, 1):
+            want, mag, ds = attend(q[i][2:, None], c.get(0, i, 0, lens[i])[:, 1:], c.get(1, i, 0, lens[i])[:, 1:], 0.125, ints([lens[i]]))
+            close(o[i][2:, None], want, mag, ds, lens[i], 2.0 ** -15, F32)
+
+
+@pytest.mark.parametrize("store,gain", [(I8, 1e-22), (I8, 1e30), (I8, 1e36), (E4M3, 1e-22), (E4M3, 1e30), (E4M3, 1e36), (BF16, 1e-22), (BF16, 1e30)])
+def test_decode_very_large_and_small_values(store, gain):
+    lens = [300, 20]
+    c, q, out, _, s = decode_case(store, F32, 4, 2, 64, 16, lens, seed=23, v_gain=lambda j: torch.where(j % 3 == 0, gain, gain / 100))
+    check_decode(c, q, out, lens, s, F32)
+
+
+def test_views_of_a_wider_page_table_and_repeated_inputs():
+    kv, hd, page = 2, 64, 16
+    c = Cache(F16, kv, hd, page, 100, 3, seed=24)
+    wide = torch.full((3, 50), -7, dtype=torch.int32, device=DEV)
+    wide[:, 11:11 + c.per] = c.table
+    h = mdi.KvCache(c.pool, wide[:, 11:11 + c.per])
+    k = torch.randn(1, kv, hd, generator=gen(1), device=DEV).expand(100, kv, hd)   # one row, a hundred times
+    v = torch.randn(100, 1, hd, generator=gen(2), device=DEV).expand(100, kv, hd)  # one head, twice
+    status = ints([0])
+    mdi.kv_append(h, k, v, starts([60, 0, 35]), ints([0, 0, 3]), status=status)    # the last five rows belong to no sequence
+    assert status.item() == 0
+    assert torch.equal(c.get(0, 0, 0, 60).float(), k[:60].half().float()) and torch.equal(c.get(1, 2, 3, 35).float(), v[60:95].half().float())
+    q = torch.randn(1, 1, hd, generator=gen(3), device=DEV).expand(3, 4, hd)
+    out = torch.empty(3, 4, hd, device=DEV)
+    ws = torch.empty(max(1, mdi.attn_decode_workspace(h, 4)), dtype=torch.uint8, device=DEV)
+    mdi.attn_decode(h, q, out, ints([60, 0, 0]), workspace=ws, status=status)
+    assert status.item() == 0
+    check_decode(c, q, out, [60, 0, 0], [0, 1, 2], F32)
+    one = torch.empty(1, kv, hd, device=DEV).expand(100, kv, hd)                   # an output whose rows are one another
+    for f in (lambda: mdi.kv_read(h, one, torch.empty(100, kv, hd, device=DEV), starts([60, 0, 35])),
+              lambda: mdi.attn_decode(h, q, torch.empty(3, 1, hd, device=DEV).expand(3, 4, hd), ints([1, 1, 1]), workspace=ws)):
+        with pytest.raises(mdi.MdiError) as e:
+            f()
+        assert e.value.code == mdi.ERR_SHAPE
+
+
+def test_calls_without_work():
+    c, q, out, ws, _ = decode_case(I8, F32, 4, 2, 64, 16, [48], seed=25)
+    before = c.raw().clone()
+    k, none, status = torch.zeros(5, 2, 64, device=DEV), ints([]), ints([0])
+    mdi.kv_append(c.handle, k, k, ints([0]), none, status=status)                  # no sequence
+    mdi.kv_append(c.handle, k[:0], k[:0], ints([0, 0]), ints([0]), status=status)  # no rows
+    o = torch.full_like(k, 4.0)
+    mdi.kv_read(c.handle, o, o.clone(), ints([0]), status=status)
+    mdi.kv_read(c.handle, o[:0], o[:0], ints([0, 0]), status=status)
+    assert (o == 4).all() and torch.equal(before, c.raw())
+    mdi.attn_decode(c.handle, q[:0], out[:0], none, status=status)
+    p = torch.full((5, 2, 64), 4.0, dtype=BF16, device=DEV)
+    mdi.attn_prompt(p, p, p, p, ints([0]), ints([0]), status=status)
+    mdi.attn_prompt(p[:0], p, p, p[:0], ints([0, 0]), ints([0, 5]), status=status)
+    assert (p == 4).all()
+    mdi.attn_prompt(p.clone(), p[:0], p[:0], p, ints([0, 5]), ints([0, 0]), status=status)   # queries without keys
+    assert (p == 0).all() and status.item() == 0
 
 
 def test_decode_is_reproducible_on_streams_and_in_graphs():
@@ -540,6 +638,56 @@ def test_prompt_bad_offsets():
         assert status.item() == mdi.STATUS_RANGE
         assert torch.equal(out[:50], good[:50])
         assert (out[50:] == 3).all()
+
+
+@pytest.mark.parametrize("n", [64, 65, 150])
+def test_prompt_of_many_sequences(n):
+    """Around the number up to which tiles are ordered over all sequences; some empty, one whose offsets do not fit."""
+    nq = [(61 * i) % 300 if i % 4 else 0 for i in range(n)]
+    nk = [x + (i * 13) % 200 for i, x in enumerate(nq)]
+    nq[n - 1], nk[n - 1] = 290, 1000
+    nk[1] = 20                                                # fewer keys than queries
+    q, k, v = prompt_case(BF16, 2, 1, 64, nq, nk, seed=n)
+    out, status = torch.full_like(q, 3.0), ints([0])
+    mdi.attn_prompt(q, k, v, out, starts(nq), starts(nk), status=status)
+    assert status.item() == 0
+    check_prompt(q, k, v, out, nq, nk, BF16)
+    ks, bad = starts(nk), torch.full_like(q, 3.0)
+    ks[n] = sum(nk) + 1                                       # the last one's keys end behind the rows
+    mdi.attn_prompt(q, k, v, bad, starts(nq), ks, status=status)
+    assert status.item() == mdi.STATUS_RANGE
+    assert torch.equal(bad[:-290], out[:-290]) and (bad[-290:] == 3).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_prompt_scores_of_minus_infinity(dtype):
+    """Keys that give -inf weigh nothing; a row that sees no others gives zeros."""
+    n = 200
+    q, k, v = prompt_case(dtype, 2, 1, 64, [n], [n], seed=6)
+    k, v = k.contiguous(), v.contiguous()
+    q[:, :, 0] = 1.0
+    k[:40, :, 0] = -math.inf
+    out = torch.empty_like(q)
+    mdi.attn_prompt(q, k, v, out, starts([n]), starts([n]))
+    assert (out[:40] == 0).all()
+    seen = torch.arange(1, n - 40 + 1, device=DEV)
+    want, mag, ds = attend(q[40:].transpose(0, 1), k[40:], v[40:], 0.125, seen)
+    close(out[40:].transpose(0, 1), want, mag, ds, n, torch.finfo(dtype).eps / 2 + 2.0 ** -15, dtype)
+
+
+def test_prompts_on_two_streams():
+    nq = [700, 33, 260]
+    q, k, v = prompt_case(BF16, 8, 2, 128, nq, nq, seed=8)
+    good = torch.empty_like(q)
+    mdi.attn_prompt(q, k, v, good, starts(nq), starts(nq))
+    qs = starts(nq)
+    streams, outs = [torch.cuda.Stream() for _ in range(2)], [torch.empty_like(q) for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for st, o in zip(streams, outs):
+            mdi.attn_prompt(q, k, v, o, qs, qs, stream=st.cuda_stream)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, good) for o in outs)
 
 
 def test_prompt_rows_past_32_bits():

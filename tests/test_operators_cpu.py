@@ -92,3 +92,17 @@ def test_prompt():
     odd = torch.zeros(7, 2, 68, dtype=BF16)[:, :, :64]
     assert code(mdi.attn_prompt, q, odd, k, q, *one) == mdi.ERR_SHAPE
     assert code(mdi.attn_prompt, q, k, k, q, *one) in (mdi.ERR_ARG, mdi.ERR_CUDA)
+
+
+def test_outputs_that_overlap_themselves():
+    c, q = make(), rows(2, 8, 64)
+    assert code(mdi.attn_decode, c, q, q[:1].expand(2, 8, 64), ints(1, 1)) == mdi.ERR_SHAPE
+    assert code(mdi.kv_read, c, rows(4, 1, 64).expand(4, 2, 64), rows(4, 2, 64), ints(0, 4), ints(0)) == mdi.ERR_SHAPE
+    k, one = rows(7, 2, 64), (ints(0, 5), ints(0, 7))
+    assert code(mdi.attn_prompt, rows(5, 4, 64), k, k, rows(1, 4, 64).expand(5, 4, 64), *one) == mdi.ERR_SHAPE
+
+
+def test_scales_whose_product_with_log2_e_overflows():
+    c, q = make(), rows(2, 8, 64)
+    assert code(mdi.attn_decode, c, q, q, ints(1, 1), scale=2.9e38) == mdi.ERR_ARG
+    assert code(mdi.attn_prompt, rows(5, 4, 64), rows(7, 2, 64), rows(7, 2, 64), rows(5, 4, 64), ints(0, 5), ints(0, 7), scale=2.9e38) == mdi.ERR_ARG
