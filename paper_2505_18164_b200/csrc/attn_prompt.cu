@@ -4,8 +4,10 @@
 // Bound: the tensor cores (4 head_dim flops per query, head and key seen) and, at head_dim 64 and close behind at 128, the
 // exponentials (one per query, head and key, 16 a clock and SM).
 //
-// A block per SM takes items one after the other: 256 query rows of one head (two sub-tiles of 128), whose keys it walks in tiles of
-// 128, once.  Its warps have their own loops over the items, so that loads and products of the next item run while the outputs of
+// A block per SM takes items one after the other: two sub-tiles of 128 query rows each, whose keys it walks in tiles of 128, once.  They
+// are the same rows of two heads where an even number of heads share a key/value head (both then see the same keys, and short
+// sequences fill both: 16 sequences of 1 to 2048 rows, 32 heads on 8, 143 instead of 149 us; 8192 rows 514 instead of 536), else 256
+// rows of one head.  Its warps have their own loops over the items, so that loads and products of the next item run while the outputs of
 // the last one are still being written (a block per item spends 9000 clocks on filling and emptying itself, three tiles' worth):
 //   warp 19     looks items up, ahead of the others;
 //   warp 16     requests the tiles by TMA (128-byte swizzle, no multicast): queries once, then keys and values through one ring;
@@ -46,7 +48,8 @@ struct ApArgs {
     OpRows v, out;
     const int *q_start, *k_start;
     int *status;
-    int n_seq, n_q, n_k, n_head, group, hd;
+    int n_seq, n_q, n_k, group, hd;
+    int tile_rows, item_heads, heads; // rows of a sequence and heads of an item; items per tile of rows
     int q_swap, k_swap, v_swap; // the tensor map has (element, row, head) instead of (element, head, row)
     float scale_log2e;
     unsigned long long wait_ns; // longest wait
@@ -61,7 +64,10 @@ template <int HDP> struct ApLayout {
     static constexpr int SMEM = BARS + 2560; // barriers and what threads tell each other
 };
 
-struct ApItem { int tile, q0, nq, k0, nk, head, kvh; }; // a tile (negative: no more items), its sequence, its head and key/value head
+struct ApItem {
+    int tile, q0, nq, k0, nk, kvh;         // a tile of a sequence (negative: no more items), the sequence, the key/value head
+    int head[2], row[2], n[2];             // of the sub-tiles: head, first row within the sequence, tiles of keys
+};
 struct ApShared { // behind the ring
     unsigned long long qfull, qempty, full[8], empty[8], sready[2], sfree, pready[4], pvdone[2], ofree[2], ifull[2], iempty[2], drain[2];
     unsigned tmem;
@@ -69,11 +75,6 @@ struct ApShared { // behind the ring
     ApItem item[2];
     float row[2][2][AP_ROWS];      // [sub-tile][half][row]: what the two threads of a row tell each other
 };
-// key tiles of sub-tile s of an item: up to what its last row sees
-__device__ __forceinline__ int ap_key_tiles(const ApItem *i, int s) {
-    const int r0 = (2 * i->tile + s) * AP_ROWS, seen = i->tile >= 0 && r0 < i->nq ? min(i->nk, i->nk - i->nq + min(r0 + AP_ROWS, i->nq)) : 0;
-    return seen > 0 ? (seen + AP_ROWS - 1) / AP_ROWS : 0;
-}
 static_assert(sizeof(ApShared) <= 2560, "ApShared");
 
 __device__ __forceinline__ void ap_init(uint32_t bar, int n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(n) : "memory"); }
@@ -194,7 +195,7 @@ template <typename T> __device__ __forceinline__ uint32_t ap_nonfinite(uint32_t 
     return std::is_same<T, __half>::value ? ((w & 0x7c007c00u) + 0x04000400u) & 0x80008000u : ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
 }
 
-// Sequence and 256-row tile of an item, x-th in the order in which tiles are taken.  One warp.  A sequence whose offsets do not
+// Sequence and tile of rows of an item, x-th in the order in which tiles are taken.  One warp.  A sequence whose offsets do not
 // fit has no tiles.  Tiles that see the most keys come first, so that no long one is left to run alone at the end: over all
 // sequences where there are at most AP_SORT (found by bisection on the number of key tiles), else sequence by sequence.
 struct ApSeq { int q0, nq, k0, nk, tiles; };
@@ -207,15 +208,15 @@ __device__ __forceinline__ ApSeq ap_seq(const ApArgs &a, int i, bool tell) {
         return s;
     }
     s.q0 = q0; s.nq = q1 - q0; s.k0 = k0; s.nk = k1 - k0;
-    s.tiles = (s.nq + 2 * AP_ROWS - 1) / (2 * AP_ROWS);
+    s.tiles = (s.nq + a.tile_rows - 1) / a.tile_rows;
     return s;
 }
-// tiles of the sequence that see at least `level` key tiles (the last ones; tile t sees the keys up to off + 256 (t + 1))
-__device__ __forceinline__ int ap_at_least(const ApSeq &s, int level) {
+// tiles of the sequence that see at least `level` key tiles (the last ones; tile t sees the keys up to off + tile_rows (t + 1))
+__device__ __forceinline__ int ap_at_least(const ApArgs &a, const ApSeq &s, int level) {
     const int keys = (level - 1) * AP_ROWS; // more than this many
     if (level <= 0) return s.tiles;
     if (s.nk <= keys || s.tiles == 0) return 0;
-    const int first = keys - (s.nk - s.nq) < 0 ? 0 : (keys - (s.nk - s.nq)) / (2 * AP_ROWS);
+    const int first = keys - (s.nk - s.nq) < 0 ? 0 : (keys - (s.nk - s.nq)) / a.tile_rows;
     return s.tiles - min(first, s.tiles - 1);
 }
 __device__ __forceinline__ int ap_sum(int n) { return __reduce_add_sync(0xffffffffu, n); }
@@ -239,9 +240,9 @@ __device__ __forceinline__ void ap_find_tile(const ApArgs &a, int x, int lane, b
         int lo = 0, hi = (__reduce_max_sync(0xffffffffu, max(s0.nk, s1.nk)) + AP_ROWS - 1) / AP_ROWS; // the largest level with more than x tiles at or above it
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
-            if (ap_sum(ap_at_least(s0, mid) + ap_at_least(s1, mid)) > x) lo = mid; else hi = mid - 1;
+            if (ap_sum(ap_at_least(a, s0, mid) + ap_at_least(a, s1, mid)) > x) lo = mid; else hi = mid - 1;
         }
-        const int a0 = ap_at_least(s0, lo), a1 = ap_at_least(s1, lo), n0 = a0 - ap_at_least(s0, lo + 1), n1 = a1 - ap_at_least(s1, lo + 1);
+        const int a0 = ap_at_least(a, s0, lo), a1 = ap_at_least(a, s1, lo), n0 = a0 - ap_at_least(a, s0, lo + 1), n1 = a1 - ap_at_least(a, s1, lo + 1);
         const int rank = x - (ap_sum(a0 + a1) - ap_sum(n0 + n1)); // among the tiles of exactly this level
         const int before = ap_scan(n0 + n1, lane) - n0 - n1;
         if (rank >= before && rank < before + n0) ap_found(it, s0, s0.tiles - a0 + rank - before);
@@ -323,10 +324,21 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             if (it >= 2 && !ap_wait_warp(b_iempty + 8 * (it & 1), ((it >> 1) & 1) ^ 1, abort, a)) break;
             const long long x = (long long)it * gridDim.x + (it & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
             ApItem *i = &sh->item[it & 1];
-            ap_find_tile(a, (int)min(x / a.n_head, (long long)0x7fffffff), lane, it == 0 && blockIdx.x == 0, i);
+            ap_find_tile(a, (int)min(x / a.heads, (long long)0x7fffffff), lane, it == 0 && blockIdx.x == 0, i);
             __syncwarp();
             const bool last = i->tile < 0;
-            if (lane == 0) { i->head = (int)(x % a.n_head); i->kvh = i->head / a.group; ap_arrive(b_ifull + 8 * (it & 1)); }
+            if (lane == 0) {
+                const int head = (int)(x % a.heads) * a.item_heads;
+                i->kvh = head / a.group;
+                for (int s = 0; s < 2; ++s) {
+                    const int row = i->tile * a.tile_rows + (a.tile_rows > AP_ROWS ? s * AP_ROWS : 0); // keys: up to what the last row sees
+                    const int seen = !last && row < i->nq ? min(i->nk, i->nk - i->nq + min(row + AP_ROWS, i->nq)) : 0, n = seen > 0 ? (seen + AP_ROWS - 1) / AP_ROWS : 0;
+                    i->head[s] = head + (a.item_heads > 1 ? s : 0);
+                    i->row[s] = row;
+                    i->n[s] = n;
+                }
+                ap_arrive(b_ifull + 8 * (it & 1));
+            }
             if (__any_sync(0xffffffffu, last)) break;
         }
     } else if (warp == 16) { // ---- TMA (lane 0; the others only keep step)
@@ -334,7 +346,8 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
         for (int it = 0;; ++it) {
             if (!arrived(it)) break;
             const ApItem *i_ = &sh->item[it & 1];
-            const int nt0 = ap_key_tiles(i_, 0), nt1 = ap_key_tiles(i_, 1), n_tiles = max(nt0, nt1), kvh = i_->kvh, head = i_->head, k0 = i_->k0, q_row = i_->q0 + i_->tile * 2 * AP_ROWS;
+            const int nt0 = i_->n[0], nt1 = i_->n[1], n_tiles = max(nt0, nt1), kvh = i_->kvh, head0 = i_->head[0], head1 = i_->head[1], k0 = i_->k0,
+                      q_row0 = i_->q0 + i_->row[0], q_row1 = i_->q0 + i_->row[1];
             const bool more = i_->tile >= 0;
             done_with(it);
             if (!more) break;
@@ -354,8 +367,8 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                     if (items > 0) ok = ap_wait_warp(b_qempty, (items - 1) & 1, abort, a);
                     if (ok && lane == 0) {
                         ap_expect(b_qfull, ((nt0 > 0) + (nt1 > 0)) * L::TILE);
-                        if (nt0 > 0) ap_load<HDP>(s_base + L::Q, &tm_q, a.q_swap, head, q_row, b_qfull);
-                        if (nt1 > 0) ap_load<HDP>(s_base + L::Q + L::TILE, &tm_q, a.q_swap, head, q_row + AP_ROWS, b_qfull);
+                        if (nt0 > 0) ap_load<HDP>(s_base + L::Q, &tm_q, a.q_swap, head0, q_row0, b_qfull);
+                        if (nt1 > 0) ap_load<HDP>(s_base + L::Q + L::TILE, &tm_q, a.q_swap, head1, q_row1, b_qfull);
                     }
                     if (ok) ++items;
                 }
@@ -377,7 +390,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             for (int it = 0; ok; ++it) {
                 ok = arrived(it);
                 if (!ok) break;
-                const int nt0 = __shfl_sync(0xffffffffu, ap_key_tiles(&sh->item[it & 1], 0), 0), nt1 = __shfl_sync(0xffffffffu, ap_key_tiles(&sh->item[it & 1], 1), 0), n_all = max(nt0, nt1);
+                const int nt0 = __shfl_sync(0xffffffffu, sh->item[it & 1].n[0], 0), nt1 = __shfl_sync(0xffffffffu, sh->item[it & 1].n[1], 0), n_all = max(nt0, nt1);
                 const bool last = __any_sync(0xffffffffu, sh->item[it & 1].tile < 0);
                 done_with(it);
                 if (last) break;
@@ -385,14 +398,13 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                 ok = ap_wait_warp(b_qfull, items++ & 1, abort, a);
                 for (int j = 0; j < n_all && ok; ++j) {
                     ok = ap_wait_warp(b_full + 8 * st, par, abort, a);
-                    const uint32_t k = base + L::RING + st * L::TILE;
 #pragma unroll
                     for (int s = 0; s < 2; ++s) {
                         if (j >= (s ? nt1 : nt0) || !ok) continue;
                         if (uses > 0) ok = ap_wait_warp<false>(b_free, (uses - 1) & 1, abort, a); // the previous scores have been taken
                         if (!ok) continue;
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                        const uint32_t q = base + L::Q + s * L::TILE;
+                        const uint32_t q = base + L::Q + s * L::TILE, k = base + L::RING + st * L::TILE;
 #pragma unroll
                         for (int e = 0; e < HDP / 16; ++e) {
                             const uint32_t o = (e / 4) * (AP_ROWS * 128) + (e % 4) * 32;
@@ -414,16 +426,16 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             for (int it = 0; ok; ++it) {
                 ok = arrived(it);
                 if (!ok) break;
-                const int nt0 = __shfl_sync(0xffffffffu, ap_key_tiles(&sh->item[it & 1], 0), 0), nt1 = __shfl_sync(0xffffffffu, ap_key_tiles(&sh->item[it & 1], 1), 0), n_all = max(nt0, nt1);
+                const int nt0 = __shfl_sync(0xffffffffu, sh->item[it & 1].n[0], 0), nt1 = __shfl_sync(0xffffffffu, sh->item[it & 1].n[1], 0), n_all = max(nt0, nt1);
                 const bool last = __any_sync(0xffffffffu, sh->item[it & 1].tile < 0);
                 done_with(it);
                 if (last) break;
                 for (int j = 0; j < n_all && ok; ++j) {
                     ok = ap_wait_warp(b_full + 8 * st, par, abort, a);
-                    const uint32_t v = base + L::RING + st * L::TILE;
 #pragma unroll
                     for (int s = 0; s < 2; ++s) {
                         if (j >= (s ? nt1 : nt0)) continue;
+                        const uint32_t v = base + L::RING + st * L::TILE;
                         if (j == 0) { // the outputs of the sub-tile's previous item have been taken
                             if (items[s] > 0) ok = ok && ap_wait_warp<false>(b_ofree + 8 * s, (items[s] - 1) & 1, abort, a);
                             ++items[s];
@@ -466,10 +478,10 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
             bool ok = arrived(it);
             const ApItem *item = &sh->item[it & 1];
             if (ap_vote(9 + s, !ok, 256) || item->tile < 0) break; // all of the sub-tile's warps go on, or none
-            const int t_end = t + ap_key_tiles(item, s);
-            int here = min(item->nk - item->nq + (2 * item->tile + s) * AP_ROWS + r + 1, item->nk) - 64 * half; // keys of this half and on that the row sees
+            const int t_end = t + item->n[s];
+            int here = min(item->nk - item->nq + item->row[s] + r + 1, item->nk) - 64 * half; // keys of this half and on that the row sees
             // first tile with a key that some row of the item does not see
-            const int t_masked = t + min(max(item->nk - item->nq + item->tile * 2 * AP_ROWS + 1, 0), item->nk) / AP_ROWS;
+            const int t_masked = t + min(max(item->nk - item->nq + item->row[0] + 1, 0), item->nk) / AP_ROWS;
             bool first = true;
             float m = -INFINITY, l = 0.f; // what the weights refer to (in log2 units), sum of this thread's weights
             for (; t < t_end; ++t, here -= AP_ROWS, ring += 2) {
@@ -591,13 +603,12 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                     l += s0 + s1;
                 }
             }
-            const int n_mine = ap_key_tiles(item, s);
-            ring += 2 * (max(ap_key_tiles(item, 0), ap_key_tiles(item, 1)) - n_mine); // the other sub-tile's
+            const int n_mine = item->n[s];
+            ring += 2 * (max(item->n[0], item->n[1]) - n_mine); // the other sub-tile's
             // ---- output: half of the columns each
-            const int seen = min(item->nk - item->nq + (2 * item->tile + s) * AP_ROWS + r + 1, item->nk);
-            const int row = (2 * item->tile + s) * AP_ROWS + r, nq = item->nq; // row of the sequence
+            const int row = item->row[s] + r, nq = item->nq, seen = min(item->nk - nq + row + 1, item->nk); // row of the sequence
             const bool valid = row < nq;
-            T *out = (T *)a.out.data + (long long)(item->q0 + row) * a.out.row_stride + (long long)item->head * a.out.head_stride;
+            T *out = (T *)a.out.data + (long long)(item->q0 + row) * a.out.row_stride + (long long)item->head[s] * a.out.head_stride;
             if (n_mine == 0) {
                 if (valid && half == 0)
                     for (int e = 0; e < a.hd; e += 8) *(uint4 *)(out + e) = make_uint4(0, 0, 0, 0);
@@ -627,7 +638,7 @@ k_attn_prompt(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ 
                         w.w = ap_pack<T>(__uint_as_float(y[e + 6]), __uint_as_float(y[e + 7]));
                         *(uint4 *)(mine + lane * 64 + ((e / 8 ^ (lane >> 1 & 3)) * 16)) = w;
                     }
-                    if (poison && valid) ap_add_nonfinite<T>(a, mine + lane * 64, lane >> 1 & 3, item->kvh, item->k0 + min(max(item->nk - item->nq + item->tile * 2 * AP_ROWS + 1, 0), item->nk) / AP_ROWS * AP_ROWS, item->k0 + seen, o);
+                    if (poison && valid) ap_add_nonfinite<T>(a, mine + lane * 64, lane >> 1 & 3, item->kvh, item->k0 + min(max(item->nk - nq + item->row[0] + 1, 0), item->nk) / AP_ROWS * AP_ROWS, item->k0 + seen, o);
                     if (o + 32 == (half + 1) * (HDP / 2)) { // the last of this warp's columns: the next item's outputs may come
                         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                         __syncwarp();
@@ -719,11 +730,15 @@ extern "C" int mdi_attn_prompt(int n_seq, const int32_t *q_start_dev, const int3
     if (e != CUDA_SUCCESS) return op_fail(MDI_ERR_SHAPE, "%s: no tensor map for these rows and strides (%d)", who, (int)e);
     a.v = op_rows(v); a.out = op_rows(out);
     a.q_start = q_start_dev; a.k_start = k_start_dev; a.status = status_dev;
-    a.n_seq = n_seq; a.n_q = n_q_rows; a.n_k = n_k_rows; a.n_head = n_head; a.group = n_head / n_kv_head; a.hd = head_dim;
+    a.n_seq = n_seq; a.n_q = n_q_rows; a.n_k = n_k_rows; a.group = n_head / n_kv_head; a.hd = head_dim;
     a.scale_log2e = scale * 1.4426950408889634f;
     a.wait_ns = AP_WAIT_NS + AP_WAIT_KEY_NS * (unsigned long long)n_k_rows;
-    const int64_t items = ((int64_t)n_q_rows / (2 * AP_ROWS) + std::min(n_seq, n_q_rows)) * n_head; // at most
-    const dim3 grid((unsigned)std::min<int64_t>(items, AP_SM));
+    const bool pair = a.group % 2 == 0;
+    a.tile_rows = pair ? AP_ROWS : 2 * AP_ROWS;
+    a.item_heads = pair ? 2 : 1;
+    a.heads = n_head / a.item_heads;
+    const int64_t tiles = (int64_t)n_q_rows / a.tile_rows + std::min(n_seq, n_q_rows); // at most
+    const dim3 grid((unsigned)std::min<int64_t>(tiles * a.heads, AP_SM));
     cudaStream_t st = (cudaStream_t)stream;
     cudaError_t ce;
     if (q->dtype == MDI_DTYPE_F16) ce = head_dim == 128 ? ap_launch<__half, 128>(mq, mk, mv, a, grid, st) : ap_launch<__half, 64>(mq, mk, mv, a, grid, st);
