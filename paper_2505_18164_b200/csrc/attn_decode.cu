@@ -22,6 +22,11 @@
 //    the planes are fp16), weights as two planes, or as one fp16 where the output is 16 bits anyway (half a step of 2^-11 against
 //    the output's own 2^-11 or 2^-8).  Weights refer to a running bound of score and value scale, so that fp16's range does not
 //    matter.  Scores, weights' sums and outputs are fp32.
+//
+// Measured with both kernels, called from a host loop (bytes of cached rows over time; a plain copy moves 6.45 TB/s): 4 x 100003 e4m3
+// rows, 40 heads on 8 of 128: 154 us, 5.5 TB/s; 64 x 640 int8 rows, 32 heads of 128: 78 us, 4.5 TB/s (68 us in the main kernel, bound by
+// its instructions: issue slots 52% busy, three warps a scheduler); 32 ragged sequences up to 8192 bf16 rows: 31 us, 3.6 TB/s; 1000
+// fp16 rows, 12 heads of 64: 14 us, all of it launches.
 #include "ops_common.cuh"
 
 #include <cuda_fp8.h>
