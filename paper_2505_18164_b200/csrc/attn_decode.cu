@@ -7,6 +7,7 @@
 //    shares, so sequences of any mix of lengths keep every warp equally busy.  A (sequence, head) that a share boundary
 //    cuts leaves partial results (maximum, sum, unnormalised output) in the workspace; a second, small kernel joins them in
 //    a fixed order.  Nothing depends on timing.
+//  * Where that leaves a warp next to nothing, a pair has a block, or a cluster of blocks, to itself instead (ad_plan).
 //  * A warp streams its tiles through its own ring of shared memory with asynchronous copies of whole contiguous rows (a
 //    unit's rows of one head are contiguous in its page).  16-byte chunks are stored swizzled, so that reading fragments has
 //    no bank conflicts where rows have 128 bytes or more.  No barrier but the warp's own is needed.
@@ -26,7 +27,7 @@
 // Measured with both kernels, called from a host loop (bytes of cached rows over time; a plain copy moves 6.45 TB/s): 4 x 100003 e4m3
 // rows, 40 heads on 8 of 128: 154 us, 5.5 TB/s; 64 x 640 int8 rows, 32 heads of 128: 78 us, 4.5 TB/s (68 us in the main kernel, bound by
 // its instructions: issue slots 52% busy, three warps a scheduler); 32 ragged sequences up to 8192 bf16 rows: 31 us, 3.6 TB/s; 1000
-// fp16 rows, 12 heads of 64: 14 us, all of it launches.
+// fp16 rows, 12 heads of 64: 11 us, most of it the host's (6 us on the device).
 #include "ops_common.cuh"
 
 #include <cuda_fp8.h>
@@ -57,6 +58,7 @@ struct AdArgs {
     float *part;      // workspace: [warps][pair from an earlier share | pair that goes on in a later one][hc][HD + 4]: output (not yet divided), what its weights refer to, their sum
     int n_seq, seq0;  // sequences of this launch, first one's number
     int n_head, group, chunks, hc, n_warps, min_tiles;
+    int whole; // blocks that a pair has to itself (a cluster), 0: tiles are dealt to warps; see ad_plan
     float scale_log2e;
 };
 
@@ -131,6 +133,15 @@ template <int ST, int UPPER> __device__ __forceinline__ uint32_t ad_wide(uint32_
 }
 template <int ST> __device__ __forceinline__ uint32_t ad_bias(uint32_t w) { return ST == AD_I8 ? w ^ 0x80808080u : w; }
 
+__device__ __forceinline__ void ad_cluster_meet() {
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float ad_remote(uint32_t addr, uint32_t rank) { // a float of block `rank` of the cluster
+    float x;
+    asm volatile("{\n .reg .b32 a;\n mapa.shared::cluster.u32 a, %1, %2;\n ld.shared::cluster.f32 %0, [a];\n}\n" : "=f"(x) : "r"(addr), "r"(rank) : "memory");
+    return x;
+}
 // 16 bytes from global to shared memory, zeros where !ok
 __device__ __forceinline__ void ad_copy16(uint32_t dst, const unsigned char *src, bool ok) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
@@ -214,10 +225,17 @@ template <int ROWS> struct AdCursor {
             if (i < n_seq) enter(s_len, i);
         }
     }
+    // this warp's part of a pair that has `warps` warps to itself
+    __device__ __forceinline__ long long part(int seq, int in_seq, int rows, int warp, int warps) {
+        i = seq; pair = in_seq; len = rows; n_tiles = ad_tiles<ROWS>(rows);
+        tile = (int)((long long)n_tiles * warp / warps);
+        at = tile;
+        return (long long)n_tiles * (warp + 1) / warps;
+    }
     // true: the next tile belongs to another pair
-    __device__ __forceinline__ bool advance(const int *s_len, int n_seq, int pairs) {
+    __device__ __forceinline__ bool advance(const int *s_len, int n_seq, int pairs, bool whole) {
         ++at;
-        if (++tile < n_tiles) return false;
+        if (++tile < n_tiles || whole) return false;
         at += AD_TURN;
         next_pair(s_len, n_seq, pairs);
         return true;
@@ -247,7 +265,7 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     // ---- lengths, places before each sequence (every block for itself)
-    {
+    if (!a.whole) {
         __shared__ long long s_sum[AD_WARPS];
         long long run = 0;
         for (int base = 0; base < a.n_seq; base += AD_THREADS) {
@@ -274,13 +292,22 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
         __syncthreads();
     }
     const int pairs = a.c.n_kv_head * a.chunks;
-    const long long T = s_pref[a.n_seq] * pairs;
-    const int W = ad_warps(a, T), w = blockIdx.x * AD_WARPS + warp;
-    if (T == 0 || w >= W) return;
-    const long long first = ad_share(T, W, w), last = ad_share(T, W, w + 1);
+    const int w = blockIdx.x * AD_WARPS + warp;
+    long long first, last;
     AdCursor<TL::ROWS> cur, nxt; // consumer, producer
-    cur.seek(s_pref, s_len, a.n_seq, pairs, first);
-    if (cur.at >= last) return;
+    if (a.whole) {
+        const int mine = blockIdx.x / a.whole, rank = blockIdx.x - mine * a.whole, i = mine / pairs, in = mine - i * pairs;
+        last = cur.part(i, in, ad_len(a, i, in == 0 && rank == 0 && tid == 0 ? a.status : nullptr), rank * AD_WARPS + warp, a.whole * AD_WARPS);
+        first = cur.at;
+    } else {
+        const long long T = s_pref[a.n_seq] * pairs;
+        const int W = ad_warps(a, T);
+        if (T == 0 || w >= W) return;
+        first = ad_share(T, W, w);
+        last = ad_share(T, W, w + 1);
+        cur.seek(s_pref, s_len, a.n_seq, pairs, first);
+        if (cur.at >= last) return;
+    }
     nxt = cur;
     int batch_i = -1, batch_tile = 0, batch_page = -1, page_slot = 0;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(ad_raw) + warp * STAGES * TL::STAGE;
@@ -338,7 +365,7 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
                 }
                 if (lane == 0) asm volatile("st.shared.s32 [%0], %1;" ::"r"(st + TL::LIVE + u * 4), "r"(rows) : "memory");
             }
-            nxt.advance(s_len, a.n_seq, pairs);
+            nxt.advance(s_len, a.n_seq, pairs, a.whole);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
@@ -528,11 +555,12 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
             }
         // ---- the end of this pair, or of this warp's share of it
         const AdCursor<TL::ROWS> was = cur;
-        const bool turn = cur.advance(s_len, a.n_seq, pairs);
+        const bool turn = cur.advance(s_len, a.n_seq, pairs, a.whole);
         if (!turn && cur.at < last) continue;
-        fresh = true;
         l += __shfl_xor_sync(0xffffffffu, l, 1);
         l += __shfl_xor_sync(0xffffffffu, l, 2);
+        if (a.whole) break;
+        fresh = true;
         const bool from_start = was.at - was.tile >= first, whole = turn && from_start; // a pair that began in an earlier share has its tile 0 there
         const int h = was.pair / a.chunks, ch = was.pair - h * a.chunks, n_here = min(AD_HC, a.group - ch * AD_HC);
         const float l0 = __shfl_sync(0xffffffffu, l, 8 * t), l1 = __shfl_sync(0xffffffffu, l, 8 * t + 4);
@@ -564,6 +592,64 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
         }
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
+    if (!a.whole) return;
+    // ---- a pair to itself: the warps' parts meet in shared memory (where the rings were) and are joined in their order; those of a
+    // cluster's blocks after that
+    float (*s_o)[AD_HC][HD + 4] = reinterpret_cast<float (*)[AD_HC][HD + 4]>(ad_raw); // [warp, then the block][head]: output, what its weights refer to, their sum
+    static_assert((AD_WARPS + 1) * AD_HC * (HD + 4) * 4 <= AD_WARPS * STAGES * TL::STAGE, "the rings hold the parts");
+    const int mine = blockIdx.x / a.whole, rank = blockIdx.x - mine * a.whole, seq = mine / pairs, in = mine - seq * pairs;
+    const int h = in / a.chunks, ch = in - h * a.chunks, n_here = min(AD_HC, a.group - ch * AD_HC);
+    const bool some = first < last;
+    __syncthreads();
+    if (some) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int k = 0; k < KS; ++k) *(float2 *)&s_o[warp][2 * t + b][TL::v_dim(g, 2 * k)] = make_float2(o[k][b], o[k][2 + b]);
+    }
+    if (t == 0) *(float2 *)&s_o[warp][g][HD] = some ? make_float2(m, l) : make_float2(-INFINITY, 0.f);
+    __syncthreads();
+    // joins `n` parts, the x-th of which is at part(x, element); -> output (not divided), reference, sum
+    auto join = [&](int n, auto part, float (&y)[(HD + 31) / 32], float &top, float &sum) {
+        top = -INFINITY;
+        sum = 0.f;
+        for (int x = 0; x < n; ++x) top = fmaxf(top, part(x, HD));
+        const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+        for (int e = 0; e < (HD + 31) / 32; ++e) y[e] = 0.f;
+        for (int x = 0; x < n; ++x) {
+            const float f = ad_exp2(part(x, HD) - ref), s = part(x, HD + 1);
+            if (s == 0.f) continue; // (nothing was seen, and no output written)
+            sum += s * f;
+#pragma unroll
+            for (int e = 0; e < (HD + 31) / 32; ++e)
+                if (HD >= 32 || lane < HD) y[e] += part(x, lane + 32 * e) * f;
+        }
+    };
+    auto store = [&](int q, const float (&y)[(HD + 31) / 32], float sum) {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        RT *out = (RT *)a.out.data + seq * a.out.row_stride + (h * a.group + ch * AD_HC + q) * a.out.head_stride;
+#pragma unroll
+        for (int e = 0; e < (HD + 31) / 32; ++e)
+            if (HD >= 32 || lane < HD) out[lane + 32 * e] = (RT)(y[e] * inv);
+    };
+    float y[(HD + 31) / 32], top, sum;
+    for (int q = warp; q < n_here; q += AD_WARPS) {
+        join(AD_WARPS, [&](int x, int e) { return s_o[x][q][e]; }, y, top, sum);
+        if (a.whole == 1) { store(q, y, sum); continue; }
+#pragma unroll
+        for (int e = 0; e < (HD + 31) / 32; ++e)
+            if (HD >= 32 || lane < HD) s_o[AD_WARPS][q][lane + 32 * e] = y[e];
+        if (lane == 0) *(float2 *)&s_o[AD_WARPS][q][HD] = make_float2(top, sum);
+    }
+    if (a.whole == 1) return;
+    ad_cluster_meet();
+    const uint32_t there = (uint32_t)__cvta_generic_to_shared(&s_o[AD_WARPS][0][0]);
+    for (int q = rank * AD_WARPS + warp; q < n_here; q += a.whole * AD_WARPS) { // the heads are shared out among all warps of the cluster
+        join(a.whole, [&](int x, int e) { return ad_remote(there + (q * (HD + 4) + e) * 4, x); }, y, top, sum);
+        store(q, y, sum);
+    }
+    ad_cluster_meet(); // nothing is read from a block that has gone
 }
 
 // Joins what the shares left of a (sequence, query head); NW warps per head, grid (heads / (4 / NW), n_seq).  Sequences without
@@ -680,7 +766,7 @@ __global__ void __launch_bounds__(AD_JOIN_THREADS) k_attn_decode_join(const AdAr
 }
 
 // ---- host --------------------------------------------------------------------------------------------------------
-struct AdPlan { int chunks, hc, n_warps, min_tiles, blocks; int64_t bytes; };
+struct AdPlan { int chunks, hc, n_warps, min_tiles, blocks, whole; int64_t bytes; };
 
 template <int HD> int ad_blocks_hd(int kv_dtype) {
     return kv_dtype == MDI_KV_I8 || kv_dtype == MDI_KV_E4M3 ? AdTile<AD_I8, HD>::BLOCKS : AdTile<AD_F16, HD>::BLOCKS;
@@ -707,6 +793,16 @@ AdPlan ad_plan(const mdi_kv_cache *c, int n_seq, int n_head, int max_len) {
     const int resident = AD_SM * ad_blocks(c) * AD_WARPS;
     p.n_warps = (int)std::max<int64_t>(1, std::min<int64_t>(resident, tiles / p.min_tiles));
     p.blocks = (p.n_warps + AD_WARPS - 1) / AD_WARPS;
+    // Few and short pairs have a cluster of 1 to 8 blocks each to themselves, joined in shared memory: one launch, no workspace, no line
+    // of tiles to find a place in.  As many blocks as leave each warp a tile and all pairs room in one wave; not with more than 4 tiles a
+    // warp, where equal shares win.  Own blocks / equal shares on the device: 12 heads of 64, f16, 128 rows 3.9 / 7.4 us, 1000 5.8 / 7.8,
+    // 4000 9.7 / 10.2; 32 heads of 128, int8, 1000 rows 8.5 / 10.3, 4000 14.1 / 16.3; 8 sequences of 32 heads on 8 of 128, bf16, 128 rows
+    // 5.0 / 10.3, 1000 12.6 / 14.0; 192 pairs of 64, 2000 rows 24.2 / 23.9.
+    const int64_t n_pairs = (int64_t)n_seq * c->n_kv_head * p.chunks, wave = AD_SM * ad_blocks(c), n_tiles = (len + rows - 1) / rows;
+    int own = 8;
+    while (own > 1 && (n_pairs * own > wave || AD_WARPS * (own / 2) >= n_tiles)) own /= 2;
+    p.whole = n_pairs * own <= wave && n_tiles <= 4 * AD_WARPS * own ? own : 0;
+    if (p.whole) return p;
     p.bytes = (int64_t)p.n_warps * 2 * p.hc * (c->head_dim + 4) * 4;
     return p;
 }
@@ -716,8 +812,22 @@ template <typename RT, int ST, int HD> cudaError_t ad_launch(const AdArgs &a, in
     static OpOnce once;
     cudaError_t e = once([] { return cudaFuncSetAttribute(k_attn_decode_op<RT, ST, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
     if (e != cudaSuccess) return e;
+    if (a.whole > 1) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(blocks);
+        cfg.blockDim = dim3(AD_THREADS);
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = st;
+        cudaLaunchAttribute at[1];
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim.x = a.whole;
+        at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+        cfg.attrs = at;
+        cfg.numAttrs = 1;
+        return cudaLaunchKernelEx(&cfg, k_attn_decode_op<RT, ST, HD>, a);
+    }
     k_attn_decode_op<RT, ST, HD><<<blocks, AD_THREADS, smem, st>>>(a);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    if ((e = cudaGetLastError()) != cudaSuccess || a.whole) return e;
     // many shares per head (few, long sequences): four warps join a head, else one
     const bool wide = a.n_warps > 8 * a.n_seq * a.c.n_kv_head * a.chunks;
     cudaLaunchConfig_t cfg = {};
@@ -780,7 +890,7 @@ extern "C" int mdi_attn_decode(const mdi_kv_cache *cache, int n_seq, const int32
     if ((rc = op_check_rows(who, "out", out, n_seq, n_head, true)) != MDI_OK) return rc;
     if (q->dtype != out->dtype) return op_fail(MDI_ERR_ARG, "%s: q and out differ in dtype", who);
     const AdPlan p = ad_plan(cache, std::max(n_seq, 1), n_head, max_len);
-    if (n_seq > 0 && (!workspace_dev || workspace_bytes < p.bytes || ((uintptr_t)workspace_dev & 15)))
+    if (p.bytes > 0 && n_seq > 0 && (!workspace_dev || workspace_bytes < p.bytes || ((uintptr_t)workspace_dev & 15)))
         return op_fail(MDI_ERR_ARG, "%s: needs a 16-byte aligned workspace of %lld bytes", who, (long long)p.bytes);
     if ((rc = op_check_ptrs(who, {{"pool_dev", cache->pool_dev, false}, {"scale_dev", cache->scale_dev, !op_scaled(cache)}, {"page_table_dev", cache->page_table_dev, false},
                                   {"q", q->data_dev, n_seq == 0}, {"out", out->data_dev, n_seq == 0}, {"slot_dev", slot_dev, true},
@@ -797,10 +907,10 @@ extern "C" int mdi_attn_decode(const mdi_kv_cache *cache, int n_seq, const int32
         a.part = (float *)workspace_dev;
         a.n_seq = std::min(AD_MAX_SEQ, n_seq - i0); a.seq0 = i0;
         a.n_head = n_head; a.group = n_head / cache->n_kv_head;
-        a.chunks = p.chunks; a.hc = p.hc; a.n_warps = p.n_warps; a.min_tiles = p.min_tiles;
+        a.chunks = p.chunks; a.hc = p.hc; a.n_warps = p.n_warps; a.min_tiles = p.min_tiles; a.whole = p.whole;
         a.scale_log2e = scale * 1.4426950408889634f;
         cudaError_t e;
-        OP_ROW_DISPATCH(q->dtype, (e = ad_store<RT>(cache->dtype, a, p.blocks, (cudaStream_t)stream)));
+        OP_ROW_DISPATCH(q->dtype, (e = ad_store<RT>(cache->dtype, a, p.whole ? a.n_seq * cache->n_kv_head * p.chunks * p.whole : p.blocks, (cudaStream_t)stream)));
         if (e != cudaSuccess) return op_cuda(who, e);
     }
     return MDI_OK;

@@ -464,6 +464,20 @@ def test_calls_without_work():
     assert (p == 0).all() and status.item() == 0
 
 
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("heads,kv,hd,n,longest", [(12, 12, 64, 1, 40), (12, 12, 64, 1, 1000), (16, 2, 128, 1, 4096), (16, 2, 128, 1, 4097), (32, 8, 128, 8, 1000),
+                                                   (5, 5, 16, 30, 512), (64, 1, 32, 3, 250), (30, 10, 128, 14, 512), (148, 148, 32, 1, 300), (148, 148, 32, 2, 300)])
+def test_decode_of_few_short_sequences(store, heads, kv, hd, n, longest):
+    """Pairs with one to eight blocks to themselves, around the sizes where that ends; a length above max_len too."""
+    lens = [longest] + [(i * 97) % (longest + 1) for i in range(1, n)]
+    for max_len in (longest, max(1, longest // 7)):
+        c, q, out, ws, s = decode_case(store, F32 if hd == 128 else F16, heads, kv, hd, 16, lens, seed=n, max_len=max_len)
+        check_decode(c, q, out, lens, s, q.dtype)
+        again = torch.empty_like(q)
+        mdi.attn_decode(c.handle, q, again, ints(lens), max_len, workspace=ws)
+        assert torch.equal(again, out.contiguous())
+
+
 def test_decode_is_reproducible_on_streams_and_in_graphs():
     lens = [3000, 700, 0, 64]
     c, q, out, ws, s = decode_case(E4M3, BF16, 32, 8, 128, 64, lens, seed=6)
