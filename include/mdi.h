@@ -328,8 +328,8 @@ int mdi_kv_read(const mdi_kv_cache *cache, int n_seq, const int32_t *slot_dev, c
  * rows of n_head heads, of the same dtype.  A sequence of which nothing is left (length 0, all its pages
  * missing) or whose scores are all -inf gives zeros; an infinity among the values gives NaN in its element of the output.  max_len: an upper bound of the lengths (0: what the page
  * table can hold); it only decides over how many blocks a sequence is split, longer sequences are still read whole.
- * workspace_dev: mdi_attn_decode_workspace() bytes (its contents do not matter), 16-byte aligned, used by one call at a
- * time.  0 < scale <= 1e38. */
+ * workspace_dev: mdi_attn_decode_workspace() bytes (its contents do not matter; NULL where that is 0), 16-byte aligned, used by
+ * one call at a time.  0 < scale <= 1e38. */
 int64_t mdi_attn_decode_workspace(const mdi_kv_cache *cache, int n_seq, int n_head, int max_len);
 int mdi_attn_decode(const mdi_kv_cache *cache, int n_seq, const int32_t *slot_dev, const int32_t *len_dev, int max_len, int n_head,
                     const mdi_rows *q, const mdi_rows *out, float scale, void *workspace_dev, int64_t workspace_bytes,

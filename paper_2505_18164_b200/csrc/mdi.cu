@@ -487,11 +487,13 @@ int kq_attention(mdi_ctx *c, Partition &P, int layer_local, const Batch *bt, int
     int rc = mdi_kv_append(&kc, bt ? T : 1, m->slot, m->start, m->pos, T, &k, &v, &m->status, st);
     if (rc == MDI_OK && bt) {
         const mdi_rows q{P.pf_qkv, MDI_DTYPE_F32, rows, s.head_dim}, o{P.obuf, MDI_DTYPE_F32, qw, s.head_dim};
-        rc = mdi_attn_decode(&kc, T, m->slot, m->len, s.n_ctx, s.n_head, &q, &o, scale, P.kq_ws, mdi_attn_decode_workspace(&kc, T, s.n_head, s.n_ctx), &m->status, st);
+        const int64_t ws = mdi_attn_decode_workspace(&kc, T, s.n_head, s.n_ctx);
+        rc = mdi_attn_decode(&kc, T, m->slot, m->len, s.n_ctx, s.n_head, &q, &o, scale, P.kq_ws, ws, &m->status, st);
         launch_k(c->pdl, k_pf_norm_split, dim3(T, ysl), dim3(PF_THREADS), 0, st, (const float *)P.obuf, qw, (int)NORM_NONE, (const float *)nullptr,
                  (const float *)nullptr, 0.f, hi, lo, (const float *)nullptr, 0, T, (const float *)nullptr, (float *)nullptr);
-        c->st.kernel_launches += c->capturing ? 0 : 5;
-        if (c->capturing) c->cap_launches += 5;
+        const int launched = ws > 0 ? 5 : 4; // (a decode attention without a workspace is one kernel, else two)
+        c->st.kernel_launches += c->capturing ? 0 : launched;
+        if (c->capturing) c->cap_launches += launched;
     } else if (rc == MDI_OK) {
         const mdi_rows kd{P.kq_k, MDI_DTYPE_F16, kw, s.head_dim}, vd{P.kq_v, MDI_DTYPE_F16, kw, s.head_dim};
         const mdi_rows q{P.kq_q, MDI_DTYPE_F16, qw, s.head_dim}, o{P.kq_o, MDI_DTYPE_F16, qw, s.head_dim};
