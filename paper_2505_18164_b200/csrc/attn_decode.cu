@@ -17,10 +17,12 @@
 //    2 (lane % 4), + 1, which is the layout that the B operand of the second product wants: A = V transposed (16 elements of
 //    head_dim x 16 rows), B = weights.  Elements of head_dim and rows are assigned to fragment positions so that all copies
 //    are wide and contiguous; both operands of a product use the same assignment.
-//  * 8-bit elements become fp16 exactly in registers (int8: a byte under the exponent of 1024, minus 1152).  Scales stay
+//  * int8 keys with few heads each (ad_launch) are multiplied as they are (m16n8k32, exact 32-bit sums): a query is then an integer of 23
+//    bits relative to the head's largest element, cut into three signed bytes, a row of A each (heads in rows 0-3, 4-7, 8-11).
+//  * Other 8-bit elements become fp16 exactly in registers (int8: a byte under the exponent of 1024, minus 1152).  Scales stay
 //    outside of the products: the key's multiplies the score, the value's the weight.
 //  * Rounding: queries are used as two 16-bit planes (high + low, 16 to 22 bits together; scaled by a power of two per head where
-//    the planes are fp16), weights as two planes, or as one fp16 where the output is 16 bits anyway (half a step of 2^-11 against
+//    the planes are fp16) or as those integers, weights as two planes, or as one fp16 where the output is 16 bits anyway (half a step of 2^-11 against
 //    the output's own 2^-11 or 2^-8).  Weights refer to a running bound of score and value scale, so that fp16's range does not
 //    matter.  Scores, weights' sums and outputs are fp32.
 //
@@ -75,6 +77,10 @@ __device__ __forceinline__ void ad_mma(float (&d)[4], const uint32_t (&a)[4], ui
 __device__ __forceinline__ void ad_mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, std::true_type) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void ad_mma(int (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ float ad_exp2(float x) {
     float y;
@@ -249,7 +255,8 @@ __device__ __forceinline__ int ad_warps(const AdArgs &a, long long T) {
     return (int)(w < 1 ? 1 : w < a.n_warps ? w : a.n_warps);
 }
 
-template <typename RT, int ST, int HD>
+// QI: int8 keys as they are (see the top of the file)
+template <typename RT, int ST, int HD, bool QI>
 __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_decode_op(const AdArgs a) {
     using TL = AdTile<ST, HD>;
     using BF = std::integral_constant<bool, AdStore<ST>::BF>;
@@ -373,7 +380,7 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
 #pragma unroll
     for (int s = 0; s < STAGES - 1; ++s) load(s);
 
-    uint32_t qa[KS][4];
+    uint32_t qa[QI ? KS / 2 : KS][4]; // queries as fragments
     float o[KS][4], m = -INFINITY, l = 0.f, q_up = 1.f; // m: what weights refer to, 2^(score - m); l: their sum
     bool fresh = true;
     int stage = 0;
@@ -381,8 +388,9 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
         if (fresh) { // a new (sequence, head, chunk): its queries, scaled into log2 units, as fragments
             fresh = false;
             const int h = cur.pair / a.chunks, ch = cur.pair - h * a.chunks;
-            const int qh = h * a.group + ch * AD_HC + g;
-            const bool there = ch * AD_HC + g < a.group;
+            const int qg = QI ? g & 3 : g; // head of the group
+            const int qh = h * a.group + ch * AD_HC + qg;
+            const bool there = ch * AD_HC + qg < a.group;
             const RT *q = (const RT *)a.q.data + cur.i * a.q.row_stride + (there ? qh : 0) * a.q.head_stride;
             float f[KS][4];
             unsigned big = 0;
@@ -405,16 +413,31 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
             if (!AdStore<ST>::BF) { // fp16 planes: the largest element to [2^12, 2^13), so that low parts stay normal numbers
                 big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
                 big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
-                if (big != 0 && big < 0x7f800000u) {
-                    const int e = min(max((int)(big >> 23) - 139, -126), 126);
+                if (big != 0 && big < 0x7f800000u) { // (QI: to [2^21, 2^22))
+                    const int e = min(max((int)(big >> 23) - (QI ? 148 : 139), -126), 126);
                     q_up = ad_pow2(e);
                     q_down = ad_pow2(-e);
+                } else if (QI && big != 0) {
+                    q_up = __uint_as_float(0x7fc00000u); // a query that is not finite: NaN
+                    q_down = 0.f;
                 }
             }
 #pragma unroll
             for (int s = 0; s < KS; ++s) {
-                ad_split(f[s][0] * q_down, f[s][1] * q_down, qa[s][0], qa[s][1], BF());
-                ad_split(f[s][2] * q_down, f[s][3] * q_down, qa[s][2], qa[s][3], BF());
+                if constexpr (QI) {
+                    uint32_t v[4], w[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int i = __float2int_rn(f[s][e] * q_down);
+                        v[e] = (uint32_t)(g < 4 ? (i + 0x8080) >> 16 : (i + 0x80) >> 8); // (its low byte counts, signed)
+                        w[e] = (uint32_t)i;
+                    }
+                    qa[s / 2][s % 2 * 2] = __byte_perm(__byte_perm(v[0], v[1], 0x0040), __byte_perm(v[2], v[3], 0x0040), 0x5410);
+                    qa[s / 2][s % 2 * 2 + 1] = g < 4 ? __byte_perm(__byte_perm(w[0], w[1], 0x0040), __byte_perm(w[2], w[3], 0x0040), 0x5410) : 0u;
+                } else {
+                    ad_split(f[s][0] * q_down, f[s][1] * q_down, qa[s][0], qa[s][1], BF());
+                    ad_split(f[s][2] * q_down, f[s][3] * q_down, qa[s][2], qa[s][3], BF());
+                }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[s][e] = 0.f;
             }
@@ -428,17 +451,24 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
         stage = stage == STAGES - 1 ? 0 : stage + 1;
 
         // ---- scores: s[2 u + r] are rows 16 u + 8 r + 2t, + 1 for head g (high part of the query, then low part)
-        float s[2 * U][4];
+        std::conditional_t<QI, int, float> s[2 * U][4];
 #pragma unroll
         for (int r = 0; r < 2 * U; ++r)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[r][e] = 0.f;
+            for (int e = 0; e < 4; ++e) s[r][e] = 0;
 #pragma unroll
         for (int c = 0; c < TL::KN; ++c) {
             constexpr int KPC = TL::KC * 4 / (TL::SZ * 16); // k-steps in a chunk
             uint32_t kw[2 * U][(TL::KC + 3) / 4];
 #pragma unroll
             for (int r = 0; r < 2 * U; ++r) ad_read<TL::KC>(kw[r], st + r / 2 * TL::UNIT + r % 2 * 8 * TL::RB + TL::at(g, TL::k_byte(t, c)));
+            if constexpr (QI) {
+#pragma unroll
+                for (int k = 0; k < KPC; k += 2)
+#pragma unroll
+                    for (int r = 0; r < 2 * U; ++r) ad_mma(s[r], qa[(c * KPC + k) / 2], kw[r][k], kw[r][k + 1]);
+                continue;
+            } else
 #pragma unroll
             for (int k = 0; k < KPC; ++k)
 #pragma unroll
@@ -468,10 +498,16 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
             vs[2 * r + 1] = v2.y;
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
-                float sum = s[r][b] + s[r][2 + b];
-                // a 16-bit key may be infinite: the low part of the query, of either sign or zero, has no say then
-                if (!SCALED && fabsf(s[r][b]) == INFINITY) sum = s[r][b];
-                x[2 * r + b] = SCALED ? sum * (b ? ks.y : ks.x) : sum;
+                if constexpr (QI) { // rows 0-3 hold the heads' highest bytes, 4-7 the middle, 8-11 the lowest
+                    const int middle = __shfl_xor_sync(0xffffffffu, s[r][b], 16);
+                    const float sum = fmaf((float)s[r][b], 65536.f, fmaf((float)middle, 256.f, (float)s[r][2 + b]));
+                    x[2 * r + b] = g < 4 ? sum * (b ? ks.y : ks.x) : 0.f;
+                } else {
+                    float sum = s[r][b] + s[r][2 + b];
+                    // a 16-bit key may be infinite: the low part of the query, of either sign or zero, has no say then
+                    if (!SCALED && fabsf(s[r][b]) == INFINITY) sum = s[r][b];
+                    x[2 * r + b] = SCALED ? sum * (b ? ks.y : ks.x) : sum;
+                }
             }
         }
         // ---- rows behind the end, or of a page that does not exist
@@ -807,10 +843,10 @@ AdPlan ad_plan(const mdi_kv_cache *c, int n_seq, int n_head, int max_len) {
     return p;
 }
 
-template <typename RT, int ST, int HD> cudaError_t ad_launch(const AdArgs &a, int blocks, cudaStream_t st) {
+template <typename RT, int ST, int HD, bool QI> cudaError_t ad_launch_as(const AdArgs &a, int blocks, cudaStream_t st) {
     constexpr size_t smem = AdTile<ST, HD>::BLOCK_SMEM;
     static OpOnce once;
-    cudaError_t e = once([] { return cudaFuncSetAttribute(k_attn_decode_op<RT, ST, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
+    cudaError_t e = once([] { return cudaFuncSetAttribute(k_attn_decode_op<RT, ST, HD, QI>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
     if (e != cudaSuccess) return e;
     if (a.whole > 1) {
         cudaLaunchConfig_t cfg = {};
@@ -824,9 +860,9 @@ template <typename RT, int ST, int HD> cudaError_t ad_launch(const AdArgs &a, in
         at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
         cfg.attrs = at;
         cfg.numAttrs = 1;
-        return cudaLaunchKernelEx(&cfg, k_attn_decode_op<RT, ST, HD>, a);
+        return cudaLaunchKernelEx(&cfg, k_attn_decode_op<RT, ST, HD, QI>, a);
     }
-    k_attn_decode_op<RT, ST, HD><<<blocks, AD_THREADS, smem, st>>>(a);
+    k_attn_decode_op<RT, ST, HD, QI><<<blocks, AD_THREADS, smem, st>>>(a);
     if ((e = cudaGetLastError()) != cudaSuccess || a.whole) return e;
     // many shares per head (few, long sequences): four warps join a head, else one
     const bool wide = a.n_warps > 8 * a.n_seq * a.c.n_kv_head * a.chunks;
@@ -840,6 +876,13 @@ template <typename RT, int ST, int HD> cudaError_t ad_launch(const AdArgs &a, in
     cfg.attrs = at;
     cfg.numAttrs = 1;
     return wide ? cudaLaunchKernelEx(&cfg, k_attn_decode_join<RT, HD, 4>, a) : cudaLaunchKernelEx(&cfg, k_attn_decode_join<RT, HD, 1>, a);
+}
+template <typename RT, int ST, int HD> cudaError_t ad_launch(const AdArgs &a, int blocks, cudaStream_t st) {
+    // int8 keys as they are, queries as integers: integers / fp16 planes 361 / 388 us for 64 x 4000 rows of 32 heads of 128 and 80 / 88 us for
+    // 12 heads of 64, one head per key head; three heads: 57 / 61 us; four (all that three rows each leave room for): 60 / 58 us
+    if constexpr (ST == AD_I8 && HD >= 32)
+        if (a.group <= 3) return ad_launch_as<RT, ST, HD, true>(a, blocks, st);
+    return ad_launch_as<RT, ST, HD, false>(a, blocks, st);
 }
 template <typename RT, int ST> cudaError_t ad_hd(const AdArgs &a, int blocks, cudaStream_t st) {
     switch (a.c.head_dim) {

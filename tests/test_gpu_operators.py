@@ -341,6 +341,22 @@ def test_decode_non_finite_rows(store):
     assert torch.isfinite(o2).all()
 
 
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("group", [1, 3, 4, 9])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_decode_queries_that_are_not_finite(store, group, bad):
+    """NaN for that head of that sequence, all others as before."""
+    lens = [300, 20]
+    c, q, out, ws, s = decode_case(store, F32, 2 * group, 2, 64, 16, lens, seed=26)
+    check_decode(c, q, out, lens, s, F32)
+    q2, o = q.clone(), torch.empty_like(q)
+    q2[0, group, 7] = bad
+    mdi.attn_decode(c.handle, q2, o, ints(lens), workspace=ws)
+    assert torch.isnan(o[0, group]).all()
+    o[0, group] = out[0, group]
+    assert torch.equal(o, out.contiguous())
+
+
 @pytest.mark.parametrize("store", [F16, BF16])
 def test_decode_scores_of_minus_infinity(store):
     """Keys that give a score of -inf weigh nothing, whether they come first or last."""
