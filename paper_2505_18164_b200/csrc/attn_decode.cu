@@ -27,8 +27,8 @@
 //    matter.  Scores, weights' sums and outputs are fp32.
 //
 // Measured with both kernels, called from a host loop (bytes of cached rows over time; a plain copy moves 6.45 TB/s): 4 x 100003 e4m3
-// rows, 40 heads on 8 of 128: 154 us, 5.5 TB/s; 64 x 640 int8 rows, 32 heads of 128: 78 us, 4.5 TB/s (68 us in the main kernel, bound by
-// its instructions: issue slots 52% busy, three warps a scheduler); 32 ragged sequences up to 8192 bf16 rows: 31 us, 3.6 TB/s; 1000
+// rows, 40 heads on 8 of 128: 154 us, 5.5 TB/s; 64 x 640 int8 rows, 32 heads of 128, fp32: 75 us, 4.6 TB/s (some 10 of them to fill and
+// empty the launch and to join); 32 ragged sequences up to 8192 bf16 rows: 31 us, 3.6 TB/s; 1000
 // fp16 rows, 12 heads of 64: 11 us, most of it the host's (6 us on the device).
 #include "ops_common.cuh"
 
@@ -77,6 +77,14 @@ __device__ __forceinline__ void ad_mma(float (&d)[4], const uint32_t (&a)[4], ui
 __device__ __forceinline__ void ad_mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, std::true_type) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// d += a (b + c), rounded to nearest
+template <typename BF> __device__ __forceinline__ void ad_mma_add(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, uint32_t c0, uint32_t c1, BF) {
+    float f[4] = {0.f, 0.f, 0.f, 0.f};
+    ad_mma(f, a, c0, c1, BF());
+    ad_mma(f, a, b0, b1, BF());
+#pragma unroll
+    for (int e = 0; e < 4; ++e) d[e] += f[e];
 }
 __device__ __forceinline__ void ad_mma(int (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -265,6 +273,10 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
     constexpr int KS = HD / 16;                       // k-steps of the scores, m-tiles of the output
     constexpr float UP = AdStore<ST>::BF ? 0.f : 10.f; // weights times value scales stay below 2^(UP + AD_SLACK): inside fp16's range, far from its end
     constexpr bool PLO = AdStore<ST>::BF || std::is_same<RT, float>::value; // low parts of the weights: see the top of the file
+    // fp32 outputs: the matrix instruction cuts off what it adds to a larger accumulator, always towards zero, so 16 rows at a time are
+    // multiplied into a fresh one and added to the output with rounding (640 int8 rows: relative error 6.7e-7 instead of 1.3e-6 for 75.2
+    // instead of 73.6 us)
+    constexpr bool RN = std::is_same<RT, float>::value;
     extern __shared__ __align__(16) unsigned char ad_raw[];
     long long *s_pref = (long long *)(ad_raw + AD_WARPS * STAGES * TL::STAGE);
     int *s_len = (int *)(s_pref + AD_MAX_SEQ + 1);
@@ -567,13 +579,16 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
                         uint32_t av[4], aw[4];
                         uint32_t y = __byte_perm(x0, x1, 0x5140), z = __byte_perm(x2, x3, 0x5140);
                         av[0] = ad_wide<ST, 0>(y); av[1] = ad_wide<ST, 1>(y); av[2] = ad_wide<ST, 0>(z); av[3] = ad_wide<ST, 1>(z);
-                        ad_mma(o[k], av, ph[2 * u], ph[2 * u + 1], BF());
+                        if constexpr (!RN) ad_mma(o[k], av, ph[2 * u], ph[2 * u + 1], BF());
                         if constexpr (TL::VC >= 4) {
                             y = __byte_perm(x0, x1, 0x7362); z = __byte_perm(x2, x3, 0x7362);
                             aw[0] = ad_wide<ST, 0>(y); aw[1] = ad_wide<ST, 1>(y); aw[2] = ad_wide<ST, 0>(z); aw[3] = ad_wide<ST, 1>(z);
-                            ad_mma(o[k + 1], aw, ph[2 * u], ph[2 * u + 1], BF());
+                            if constexpr (!RN) ad_mma(o[k + 1], aw, ph[2 * u], ph[2 * u + 1], BF());
                         }
-                        if constexpr (PLO) {
+                        if constexpr (RN) {
+                            ad_mma_add(o[k], av, ph[2 * u], ph[2 * u + 1], pl[2 * u], pl[2 * u + 1], BF());
+                            if constexpr (TL::VC >= 4) ad_mma_add(o[k + 1], aw, ph[2 * u], ph[2 * u + 1], pl[2 * u], pl[2 * u + 1], BF());
+                        } else if constexpr (PLO) {
                             ad_mma(o[k], av, pl[2 * u], pl[2 * u + 1], BF());
                             if constexpr (TL::VC >= 4) ad_mma(o[k + 1], aw, pl[2 * u], pl[2 * u + 1], BF());
                         }
@@ -584,8 +599,12 @@ __global__ void __launch_bounds__(AD_THREADS, AdTile<ST, HD>::BLOCKS) k_attn_dec
                         av[1] = __byte_perm(vw[0][i], vw[1][i], 0x7632);
                         av[2] = __byte_perm(vw[2][i], vw[3][i], 0x5410);
                         av[3] = __byte_perm(vw[2][i], vw[3][i], 0x7632);
-                        ad_mma(o[k], av, ph[2 * u], ph[2 * u + 1], BF());
-                        if constexpr (PLO) ad_mma(o[k], av, pl[2 * u], pl[2 * u + 1], BF());
+                        if constexpr (RN) {
+                            ad_mma_add(o[k], av, ph[2 * u], ph[2 * u + 1], pl[2 * u], pl[2 * u + 1], BF());
+                        } else {
+                            ad_mma(o[k], av, ph[2 * u], ph[2 * u + 1], BF());
+                            if constexpr (PLO) ad_mma(o[k], av, pl[2 * u], pl[2 * u + 1], BF());
+                        }
                     }
                 }
             }
