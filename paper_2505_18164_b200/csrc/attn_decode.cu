@@ -42,7 +42,7 @@ namespace {
 
 constexpr int AD_WARPS = 4;      // warps per block (they share nothing but the table of lengths)
 constexpr int AD_THREADS = AD_WARPS * 32;
-constexpr int AD_UNITS = 2;      // 16-row units per tile: one softmax step serves 32 rows.  16 rows: 86 instead of 78 us (int8, 32 x 128 heads, 16 x 2600 rows), 39 instead of 32 us (bf16, 40 heads on 8, 64 ragged sequences)
+constexpr int AD_UNITS = 2;      // 16-row units per tile: one softmax step serves 32 rows.  16 rows: 86 instead of 78 us (64 x 640 int8 rows, 32 heads of 128), 39 instead of 32 us (32 ragged sequences up to 8192 bf16 rows, 32 heads on 8)
 constexpr int AD_STAGES = 2;     // tiles in a warp's ring.  3 leave room for fewer blocks: 4 to 9% slower
 constexpr int AD_MAX_BLOCKS = 4; // resident blocks per SM
 constexpr int AD_MAX_SEQ = 256;  // sequences per launch (their table shares shared memory with the rings of 4 blocks per SM)
